@@ -360,6 +360,211 @@ tg_status tg_kv_restore(const void* store, size_t store_bytes, const uint64_t* c
                         const uint32_t* bytes, int n, void* kv_dst, size_t kv_bytes,
                         uint8_t* status, void* stream);
 
+/*
+ * Operators of an attention worker's speculative decode step around a paged
+ * KV cache: several tokens are drafted per request and checked in one
+ * forward, so that the expert weights streamed for it serve more rows. In
+ * order: tg_kv_pages_reserve (rows for the new tokens), per layer
+ * tg_qk_norm_rope and tg_tree_attention (and the expert layer above),
+ * tg_verify_tree, tg_kv_compact and tg_kv_pages_trim.
+ *
+ * Request b's new tokens are rows q_offsets[b] .. q_offsets[b+1]-1 (device
+ * array [B+1], non-decreasing, from 0 to T). They are the nodes of a tree:
+ * node 0, the root, is the last token already sampled; every other node is a
+ * drafted token, parents before children. tree_mask [T, W] uint64
+ * (W = mask_words, at most TG_MAX_NODES / 64) holds for each row the nodes
+ * of its request that it sees: its ancestors and itself (bit j % 64 of word
+ * j / 64). NULL means a chain: node i sees nodes 0 .. i. lengths [B] are the
+ * tokens already in the cache; node j's keys and values lie at position
+ * lengths[b] + j.
+ */
+#define TG_MAX_NODES 1024
+
+#define TG_BF16 0
+#define TG_F16 1
+
+/*
+ * A paged KV cache. Position p of request b lies in row p % page_size of
+ * page page_table[b, p / page_size]; row r of page g of layer l is the
+ * Hkv * D elements at k (and v) + l * layer_stride + g * page_stride +
+ * r * Hkv * D, so one token's K and V of a layer are one segment each (see
+ * tg_kv_checkpoint). K and V may share one allocation (each page's V after
+ * its K, with twice the stride). held [B] counts the pages of each table
+ * row, refcount [n_pages] the rows that hold a page: 0 = free. Both are kept
+ * by the tg_kv_pages_* calls and not read by the others (where they may be
+ * NULL). Entries of the table outside [0, n_pages) are never followed: such
+ * positions are neither read nor written.
+ *
+ * Limits: page_size a power of two up to 1024, D 64, 128 or 256,
+ * n_pages * page_size < 2^31, B <= 4096, k, v 16-byte aligned, strides
+ * multiples of 8 elements, page_stride >= page_size * Hkv * D.
+ */
+typedef struct {
+  int dtype; /* TG_BF16 or TG_F16 */
+  int n_layers, n_pages, page_size, Hkv, D, B, max_pages;
+  int64_t layer_stride; /* elements */
+  int64_t page_stride;  /* elements */
+  void* k;
+  void* v;
+  int32_t* page_table; /* [B, max_pages] */
+  int32_t* held;       /* [B] */
+  int32_t* refcount;   /* [n_pages] */
+} tg_kv_cache;
+
+/*
+ * Norms of queries and keys for each head, their rotation by the row's
+ * position, and the new rows' place in the cache, in one pass.
+ *
+ * Row t of qkv (qkv_stride elements from row to row) holds Hq query, Hkv key
+ * and Hkv value heads of D elements. A query or key head x becomes
+ *   y = x * rsqrt(sum(x^2) / D + eps) * weight      (q_weight, k_weight [D];
+ *                                                    both NULL: y = x)
+ * and its first rot elements turn by the angles of positions[t]:
+ * (a, b) -> (a cos - b sin, b cos + a sin) for the pairs (y[i], y[i + rot/2]),
+ * or (y[2i], y[2i+1]) if interleaved; cos_sin [max_pos, rot] float32 holds
+ * cos of the rot/2 angles, then sin. All in float32, rounded once. Queries go
+ * to q_out [T, Hq, D] (q_out_stride from row to row; may be qkv itself, in
+ * place), keys and (unchanged) values to row slots[t] % page_size of page
+ * slots[t] / page_size of the cache. Rows with a slot outside the cache (-1)
+ * are not cached; positions are clamped to [0, max_pos). rot is 0 or a
+ * multiple of 16 up to D; strides are multiples of 8 elements.
+ */
+typedef struct {
+  tg_kv_cache cache;
+  int layer, T, Hq, rot, interleaved, max_pos;
+  float eps;
+  int64_t qkv_stride, q_out_stride;
+  const void* qkv;
+  const void* q_weight;
+  const void* k_weight;
+  const float* cos_sin;
+  const int32_t* positions; /* [T] */
+  const int32_t* slots;     /* [T] */
+  void* q_out;
+} tg_qk_args;
+
+tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
+
+/*
+ * Attention of every row over its request's cached tokens and the nodes that
+ * its tree mask shows it:
+ *   out[r, h] = sum_p softmax_p(scale * q[r, h] . k[p, h / G]) * v[p, h / G]
+ * over p in [0, lengths[b]) and lengths[b] + j for the nodes j seen, with
+ * G = Hq / Hkv. Scores, the softmax's maximum and sum and the output's sums
+ * are float32; probabilities are rounded to the cache's type for their
+ * product with v. A row that sees nothing gives zeros. Positions that a row
+ * does not see do not reach it, whatever they hold (infinities and NaN
+ * included). max_nodes bounds the nodes per request (rows beyond it are not
+ * written); positions beyond the page table are not there. The work is dealt
+ * evenly over the device whatever the lengths; a request's last bits may
+ * depend on the others of its batch, but not on the run.
+ */
+typedef struct {
+  tg_kv_cache cache;
+  int layer, T, Hq, max_nodes, mask_words;
+  float scale;
+  int64_t q_stride, out_stride; /* elements from row to row, multiples of 8 */
+  const void* q;
+  const int32_t* q_offsets;  /* [B+1] */
+  const int32_t* lengths;    /* [B] */
+  const uint64_t* tree_mask; /* [T, mask_words], or NULL */
+  void* out;
+} tg_tree_attn_args;
+
+size_t tg_tree_attention_workspace(const tg_tree_attn_args* a);
+tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Which drafted tokens stay, and the token that follows them.
+ *
+ * target_probs [T, V] float32 (rows target_stride apart) is the target's
+ * distribution after each node, tokens [T] the drafted token at each node
+ * (the root's is not read). A node's parent is the highest node below it in
+ * its tree_mask row; children are looked at in order. Probabilities count in
+ * units of 2^-36 (floor, clamped to [0, 1], NaN = 0) and u in units of 2^-24
+ * (floor, clamped to [0, 1)), so that sums are exact and one answer follows:
+ *   draft_probs NULL: child j of node v, token x, stays iff
+ *     u_accept[j] * (1 - p of v's earlier children) < p_v(x);
+ *     the token after the last node kept is drawn from p there without its
+ *     children's tokens;
+ *   draft_probs [T, V] (the distribution that each node's child was sampled
+ *     from; only a node's first child is looked at): it stays iff
+ *     u_accept[j] * q_v(x) < p_v(x); after a refusal the next token is drawn
+ *     from max(p - q, 0), else from p.
+ * Drawn: the lowest token whose cumulative mass exceeds u_next[b] * the whole
+ * mass, in token order; if no mass is left, from p there as it is, and if
+ * that has none, token 0. Tokens outside [0, V) are not kept; of two children
+ * with one token the second is not. Rows sum to at most about 1 (8 at most).
+ * At most max_path nodes are kept, the root among them: deeper ones are
+ * ignored. Outputs, for request b: n_out[b] = kept nodes (0 if it has no
+ * rows), path [B, max_path] their numbers in order (0 first, then -1),
+ * tokens_out [B, max_path] the tokens after each of them: the drafted ones
+ * kept, then the one drawn (then -1).
+ */
+typedef struct {
+  int B, T, V, max_path, max_nodes, mask_words;
+  int64_t target_stride, draft_stride; /* elements from row to row */
+  const float* target_probs;
+  const float* draft_probs; /* or NULL */
+  const int32_t* tokens;    /* [T] */
+  const float* u_accept;    /* [T] */
+  const float* u_next;      /* [B] */
+  const int32_t* q_offsets; /* [B+1] */
+  const uint64_t* tree_mask;
+  int32_t* tokens_out;
+  int32_t* path;
+  int32_t* n_out;
+} tg_verify_args;
+
+size_t tg_verify_tree_workspace(const tg_verify_args* a);
+tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The rows kept by tg_verify_tree moved together: in every layer, K and V of
+ * position lengths[b] + path[b, i] go to lengths[b] + i for i < n_keep[b]
+ * (path [B, max_path] ascending with path[b, i] >= i, as tg_verify_tree
+ * writes it; entries that are not are skipped), and
+ * new_lengths[b] = lengths[b] + n_keep[b] (another array than lengths).
+ */
+tg_status tg_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
+                        const int32_t* n_keep, const int32_t* lengths, int32_t* new_lengths,
+                        void* stream);
+
+/*
+ * Pages for new rows: request b gets pages until its row holds lengths[b] +
+ * q_offsets[b+1] - q_offsets[b] tokens, in request order and the lowest free
+ * page first; from the first request on for which too few pages are free, none
+ * that needs pages gets any, and a request whose row of the table is too short
+ * gets and takes none (status[b] 0 instead of 1). slots [T] is where each new
+ * row goes in the cache (page * page_size + row), -1 where its request got no
+ * pages. A request may already hold the pages that it needs.
+ */
+tg_status tg_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
+                              const int32_t* q_offsets, int T, int32_t* slots, int32_t* status,
+                              void* stream);
+
+/*
+ * n requests forked: request dst[i], which holds no pages, becomes a copy of
+ * request src[i] with lengths[src[i]] tokens. Whole pages are shared (their
+ * reference counts grow); the rows in use of a part page are copied in every
+ * layer to a fresh page, lowest free page first, in the order of the list.
+ * status[i]: 1 done; 0 not done (too few free pages for this and all earlier
+ * forks, an index outside [0, B), dst[i] holds pages or occurs earlier in the
+ * list, src[i] occurs as a dst or holds fewer pages than its length). n is at
+ * most TG_MAX_FORKS.
+ */
+#define TG_MAX_FORKS 1024
+tg_status tg_kv_pages_fork(const tg_kv_cache* c, int32_t* lengths, const int32_t* src,
+                           const int32_t* dst, int n, int32_t* status, void* stream);
+
+/*
+ * Pages given back: request b keeps the pages of its first keep[b] tokens;
+ * the others leave its row (-1) and their reference counts drop, to 0 for
+ * pages that nobody else holds, which are then free. keep[b] = 0 releases the
+ * request.
+ */
+tg_status tg_kv_pages_trim(const tg_kv_cache* c, const int32_t* keep, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

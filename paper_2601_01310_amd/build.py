@@ -25,8 +25,8 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
           "-munsafe-fp-atomics"]
 
 SOURCES = ["gate_topk.hip", "dispatch.hip", "grouped_gemm.hip", "combine.hip", "trigger.hip",
-           "kv_checkpoint.hip", "noalloc.hip",
-           "tg_api.cpp"]
+           "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip", "tree_attention.hip",
+           "verify_tree.hip", "kv_pages.hip", "kv_api.cpp", "tg_api.cpp"]
 
 
 def _compile(src: str) -> str:

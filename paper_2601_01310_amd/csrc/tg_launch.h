@@ -136,4 +136,20 @@ hipError_t launch_kv_restore(const void* store, size_t store_bytes, const uint64
                              const uint32_t* bytes, int n, void* kv, size_t kv_bytes,
                              uint8_t* status, hipStream_t stream);
 
+// The operators around the paged KV cache (kv_api.cpp validates).
+hipError_t launch_qk_norm_rope(const tg_qk_args* a, hipStream_t stream);
+size_t tree_attention_workspace_bytes(const tg_tree_attn_args* a);
+hipError_t launch_tree_attention(const tg_tree_attn_args* a, void* ws, hipStream_t stream);
+size_t verify_workspace_bytes(const tg_verify_args* a);
+hipError_t launch_verify_tree(const tg_verify_args* a, void* ws, hipStream_t stream);
+hipError_t launch_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
+                             const int32_t* n_keep, const int32_t* lengths, int32_t* new_lengths,
+                             hipStream_t stream);
+hipError_t launch_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
+                                   const int32_t* q_offsets, int T, int32_t* slots, int32_t* status,
+                                   hipStream_t stream);
+hipError_t launch_kv_pages_fork(const tg_kv_cache* c, int32_t* lengths, const int32_t* src,
+                                const int32_t* dst, int n, int32_t* status, hipStream_t stream);
+hipError_t launch_kv_pages_trim(const tg_kv_cache* c, const int32_t* keep, hipStream_t stream);
+
 }  // namespace tg

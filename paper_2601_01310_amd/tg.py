@@ -23,7 +23,9 @@ EXPORTS = [
     "tg_remap_dispatch", "tg_expert_ffn_grouped", "tg_set_gemm_tile_policy", "tg_combine",
     "tg_ew_forward_workspace", "tg_ew_forward", "tg_ew_forward_timed", "tg_ew_forward_noalloc",
     "tg_ew_replay_workspace", "tg_ew_replay", "tg_batch_trigger", "tg_kv_checkpoint",
-    "tg_kv_checkpoint_strided", "tg_kv_restore",
+    "tg_kv_checkpoint_strided", "tg_kv_restore", "tg_qk_norm_rope", "tg_tree_attention_workspace",
+    "tg_tree_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_kv_compact",
+    "tg_kv_pages_reserve", "tg_kv_pages_fork", "tg_kv_pages_trim",
 ]
 
 
@@ -53,6 +55,46 @@ class ReplayArgs(ctypes.Structure):
             "x", "ert", "slot_alive", "w13", "w2", "topk_ids", "topk_w", "pair_slot", "pair_row",
             "y", "out", "replay_slot", "n_replayed", "n_unserved")
     ]
+
+
+def _fields(kinds):
+    """(name, ctypes type) pairs from "kind: names" lines in C order."""
+    types = dict(int=ctypes.c_int, i64=ctypes.c_int64, float=ctypes.c_float, ptr=ctypes.c_void_p)
+    return [(n, types[k]) for k, names in kinds for n in names.split()]
+
+
+class KvCacheArgs(ctypes.Structure):
+    """Mirror of ``tg_kv_cache``."""
+    _fields_ = _fields([
+        ("int", "dtype n_layers n_pages page_size Hkv D B max_pages"),
+        ("i64", "layer_stride page_stride"), ("ptr", "k v page_table held refcount")])
+
+
+class QkArgs(ctypes.Structure):
+    """Mirror of ``tg_qk_args``."""
+    _fields_ = [("cache", KvCacheArgs)] + _fields([
+        ("int", "layer T Hq rot interleaved max_pos"), ("float", "eps"),
+        ("i64", "qkv_stride q_out_stride"),
+        ("ptr", "qkv q_weight k_weight cos_sin positions slots q_out")])
+
+
+class TreeAttnArgs(ctypes.Structure):
+    """Mirror of ``tg_tree_attn_args``."""
+    _fields_ = [("cache", KvCacheArgs)] + _fields([
+        ("int", "layer T Hq max_nodes mask_words"), ("float", "scale"),
+        ("i64", "q_stride out_stride"), ("ptr", "q q_offsets lengths tree_mask out")])
+
+
+class VerifyArgs(ctypes.Structure):
+    """Mirror of ``tg_verify_args``."""
+    _fields_ = _fields([
+        ("int", "B T V max_path max_nodes mask_words"), ("i64", "target_stride draft_stride"),
+        ("ptr", "target_probs draft_probs tokens u_accept u_next q_offsets tree_mask tokens_out "
+                "path n_out")])
+
+
+BF16, F16 = 0, 1
+MAX_NODES = 1024  # TG_MAX_NODES in tg.h
 
 
 def load(path: Optional[str] = None):
@@ -105,6 +147,21 @@ def load(path: Optional[str] = None):
                                              vp, vp]
     lib.tg_kv_restore.restype = i
     lib.tg_kv_restore.argtypes = [vp, sz, vp, vp, vp, vp, vp, i, vp, sz, vp, vp]
+    kv = ctypes.POINTER(KvCacheArgs)
+    lib.tg_qk_norm_rope.restype = i
+    lib.tg_qk_norm_rope.argtypes = [ctypes.POINTER(QkArgs), vp]
+    for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_verify_tree", VerifyArgs)):
+        size, call = getattr(lib, name + "_workspace"), getattr(lib, name)
+        size.restype, size.argtypes = sz, [ctypes.POINTER(args)]
+        call.restype, call.argtypes = i, [ctypes.POINTER(args), vp, sz, vp]
+    lib.tg_kv_compact.restype = i
+    lib.tg_kv_compact.argtypes = [kv, vp, i, vp, vp, vp, vp]
+    lib.tg_kv_pages_reserve.restype = i
+    lib.tg_kv_pages_reserve.argtypes = [kv, vp, vp, i, vp, vp, vp]
+    lib.tg_kv_pages_fork.restype = i
+    lib.tg_kv_pages_fork.argtypes = [kv, vp, vp, vp, i, vp, vp]
+    lib.tg_kv_pages_trim.restype = i
+    lib.tg_kv_pages_trim.argtypes = [kv, vp, vp]
     _lib = lib
     return lib
 
@@ -269,6 +326,48 @@ def tg_kv_restore(store, store_bytes, commit, seq, src, dst, nbytes, n, kv_dst, 
     _check(load().tg_kv_restore(_flag_ptr(store), store_bytes, _flag_ptr(commit), _p(seq), _p(src),
                                 _p(dst), _p(nbytes), n, _p(kv_dst), kv_bytes, _p(status),
                                 _stream(stream)), "tg_kv_restore")
+
+
+def tg_qk_norm_rope(args: QkArgs, stream=None):
+    _check(load().tg_qk_norm_rope(ctypes.byref(args), _stream(stream)), "tg_qk_norm_rope")
+
+
+def tg_tree_attention_workspace(args: TreeAttnArgs) -> int:
+    return int(load().tg_tree_attention_workspace(ctypes.byref(args)))
+
+
+def tg_tree_attention(args: TreeAttnArgs, ws, ws_bytes, stream=None):
+    _check(load().tg_tree_attention(ctypes.byref(args), _p(ws), ws_bytes, _stream(stream)),
+           "tg_tree_attention")
+
+
+def tg_verify_tree_workspace(args: VerifyArgs) -> int:
+    return int(load().tg_verify_tree_workspace(ctypes.byref(args)))
+
+
+def tg_verify_tree(args: VerifyArgs, ws, ws_bytes, stream=None):
+    _check(load().tg_verify_tree(ctypes.byref(args), _p(ws), ws_bytes, _stream(stream)),
+           "tg_verify_tree")
+
+
+def tg_kv_compact(cache: KvCacheArgs, path, max_path, n_keep, lengths, new_lengths, stream=None):
+    _check(load().tg_kv_compact(ctypes.byref(cache), _p(path), max_path, _p(n_keep), _p(lengths),
+                                _p(new_lengths), _stream(stream)), "tg_kv_compact")
+
+
+def tg_kv_pages_reserve(cache: KvCacheArgs, lengths, q_offsets, T, slots, status, stream=None):
+    _check(load().tg_kv_pages_reserve(ctypes.byref(cache), _p(lengths), _p(q_offsets), T, _p(slots),
+                                      _p(status), _stream(stream)), "tg_kv_pages_reserve")
+
+
+def tg_kv_pages_fork(cache: KvCacheArgs, lengths, src, dst, n, status, stream=None):
+    _check(load().tg_kv_pages_fork(ctypes.byref(cache), _p(lengths), _p(src), _p(dst), n,
+                                   _p(status), _stream(stream)), "tg_kv_pages_fork")
+
+
+def tg_kv_pages_trim(cache: KvCacheArgs, keep, stream=None):
+    _check(load().tg_kv_pages_trim(ctypes.byref(cache), _p(keep), _stream(stream)),
+           "tg_kv_pages_trim")
 
 
 def _flag_ptr(t):
