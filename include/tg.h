@@ -396,7 +396,8 @@ tg_status tg_kv_restore(const void* store, size_t store_bytes, const uint64_t* c
  * positions are neither read nor written.
  *
  * Limits: page_size a power of two up to 1024, D 64, 128 or 256,
- * n_pages * page_size < 2^31, B <= 4096, k, v 16-byte aligned, strides
+ * n_pages * page_size < 2^31, max_pages * page_size <= 2^30, B <= 4096,
+ * Hkv <= 1024, k, v 16-byte aligned, strides
  * multiples of 8 elements, page_stride >= page_size * Hkv * D.
  */
 typedef struct {
