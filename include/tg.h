@@ -456,10 +456,10 @@ tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
  * product with v. A row that sees nothing gives zeros. Positions that a row
  * does not see do not reach it, whatever they hold (infinities and NaN
  * included). max_nodes bounds the nodes per request (rows beyond it are not
- * written; B * max_nodes * Hq < 2^31); positions beyond the page table are
- * not there. The work is dealt
+ * written); positions beyond the page table are not there. The work is dealt
  * evenly over the device whatever the lengths; a request's last bits may
- * depend on the others of its batch, but not on the run.
+ * depend on the others of its batch, but not on the run. Limit:
+ * B * Hkv * (max_nodes * G / 16 + 1) * (max_pages * page_size / 64) < 2^31.
  */
 typedef struct {
   tg_kv_cache cache;

@@ -103,13 +103,22 @@ __device__ __forceinline__ float inverse(float sum) {
   return sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
 }
 
+// A block's share in joining an item that several blocks had: entry 0 of a
+// block for the item that it went on with, entry 1 for the one that it began.
+struct Split {
+  int parts;  // 0: there is none
+  int at;     // this block's number among the parts
+  int k0, slot;  // the first part: block, and its slot there (then slot 0s)
+  int first, lines, g, row0;
+};
+
 struct Params {
   const uint16_t *q, *k, *v;
   int64_t q_stride, out_stride, page_stride;
   uint16_t* out;
-  int64_t* plan;    // [B + 1] units before each request, then units per block
-  float* part;      // [2 * blocks][rows][D] float32
-  float2* part_ml;  // [2 * blocks][rows] maximum and sum
+  Split* split;         // [blocks][2]
+  float* part;          // [2 * blocks][rows][D] float32
+  float2* part_ml;      // [2 * blocks][rows] maximum and sum
   int page_shift, n_pages, max_pages, words, B, T, max_nodes, Hkv, G;
   float c;
 };
@@ -134,91 +143,149 @@ __device__ __forceinline__ Request request_of(const Params& p, const int32_t* __
   return r;
 }
 
-// Units before each request, pre [B + 1]; returns this block's run of units.
-// Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
-struct Run {
-  int64_t begin, stop;
-  int me;
-};
-
-template <int kRows, int kUnit>
-__device__ __forceinline__ Run deal(const Params& p, const int32_t* __restrict__ off,
-                                    const int32_t* __restrict__ lengths, int64_t* pre,
-                                    int64_t* carry) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int64_t base = 0;
-  for (int b0 = 0; b0 < p.B; b0 += kBlock) {
-    const int b = b0 + threadIdx.x;
-    int64_t x = 0;
-    if (b < p.B) {
-      const Request r = request_of<kRows, kUnit>(p, off, lengths, b);
-      x = (int64_t)r.units * r.tiles * p.Hkv;
-    }
-#pragma unroll
-    for (int m = 1; m < kWave; m *= 2) {
-      const int64_t o = __shfl_up(x, m);
-      if (lane >= m) x += o;
-    }
-    __syncthreads();
-    if (lane == kWave - 1) carry[wave] = x;
-    __syncthreads();
-    int64_t before = base;
-    for (int i = 0; i < kWaves; ++i) {
-      if (i < wave) before += carry[i];
-      base += carry[i];
-    }
-    if (b < p.B) pre[b + 1] = before + x;
-  }
-  if (threadIdx.x == 0) pre[0] = 0;
-  __syncthreads();
-  const int64_t total = pre[p.B];
-  const int blocks = gridDim.x;
-  Run run;
-  run.me = (blockIdx.x % 8) * (blocks / 8) + blockIdx.x / 8;
-  const int64_t share = max((int64_t)1, (total + blocks - 1) / blocks);
-  if (blockIdx.x == 0) {
-    for (int b = threadIdx.x; b <= p.B; b += kBlock) p.plan[b] = pre[b];
-    if (threadIdx.x == 0) p.plan[p.B + 1] = share;
-  }
-  run.begin = run.me * share;
-  run.stop = min(total, run.begin + share);
-  return run;
-}
-
-// The piece of a run that starts at unit `at`: one item, units [u0, u1).
+// The piece of a block's run of units that starts at one of them: units [u0,
+// u1) of one item.
 struct Piece {
   Request r;
   int b, g, rt, u0, u1;
   bool whole;
 };
 
+// Deals the units to the blocks in equal runs; the units before each request
+// are kept in LDS. Up to 64 requests are summed in the lanes of each wave, so
+// that the first piece needs one round of loads.
 template <int kRows, int kUnit>
-__device__ __forceinline__ Piece piece_at(const Params& p, const int32_t* __restrict__ off,
-                                          const int32_t* __restrict__ lengths, const int64_t* pre,
-                                          int64_t at, int64_t stop) {
-  Piece x;
-  int b = 0;
-  for (int hi = p.B; hi - b > 1;) {  // the last request that starts at or before `at`
-    const int mid = (b + hi) / 2;
-    if (pre[mid] <= at) b = mid;
-    else hi = mid;
+struct Dealer {
+  const Params& p;
+  const int32_t* __restrict__ off;
+  const int32_t* __restrict__ lengths;
+  int* pre;  // LDS, [B + 1]
+  int begin, stop, share, me;
+
+  __device__ __forceinline__ Dealer(const Params& p_, const int32_t* __restrict__ off_,
+                                    const int32_t* __restrict__ lengths_, int* pre_)
+      : p(p_), off(off_), lengths(lengths_), pre(pre_) {}
+
+  __device__ __forceinline__ void runs(int total) {
+    const int blocks = gridDim.x;
+    // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
+    me = (blockIdx.x % 8) * (blocks / 8) + blockIdx.x / 8;
+    share = max(1, (total + blocks - 1) / blocks);
+    begin = (int)min((int64_t)total, (int64_t)me * share);
+    stop = min(total, begin + share);
   }
-  x.b = uniform(b);
-  x.r = request_of<kRows, kUnit>(p, off, lengths, x.b);
-  const int64_t rest = at - pre[b];
-  const int item = (int)(rest / x.r.units), u0 = (int)(rest - (int64_t)item * x.r.units);
-  x.u0 = uniform(u0);
-  x.u1 = uniform((int)min((int64_t)x.r.units, u0 + (stop - at)));
-  x.g = uniform(item / x.r.tiles);
-  x.rt = uniform(item % x.r.tiles);
-  x.r.first = uniform(x.r.first);
-  x.r.n = uniform(x.r.n);
-  x.r.L = uniform(x.r.L);
-  x.r.end = uniform(x.r.end);
-  x.r.units = uniform(x.r.units);
-  x.whole = x.u0 == 0 && x.u1 == x.r.units;
-  return x;
-}
+
+  // The block's first piece; begin == stop if it has none.
+  __device__ __forceinline__ Piece first(int* carry) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    if (p.B <= kWave) {
+      const Request mine = request_of<kRows, kUnit>(p, off, lengths, min(lane, p.B - 1));
+      const int units = lane < p.B ? mine.units * mine.tiles * p.Hkv : 0;
+      int sum = units;
+#pragma unroll
+      for (int m = 1; m < kWave; m *= 2) {
+        const int o = __shfl_up(sum, m);
+        if (lane >= m) sum += o;
+      }
+      const int before = sum - units;
+      if (wave == 0 && lane < p.B) pre[lane + 1] = sum;
+      if (threadIdx.x == 0) pre[0] = 0;
+      runs(__builtin_amdgcn_readlane(sum, kWave - 1));
+      // The last lane with units whose request starts at or before `begin`.
+      const uint64_t m = __ballot(before <= begin && units > 0);
+      Piece x;
+      x.b = m ? 63 - __clzll(m) : 0;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, x.b); };
+      x.r.first = of(mine.first);
+      x.r.n = of(mine.n);
+      x.r.L = of(mine.L);
+      x.r.end = of(mine.end);
+      x.r.units = of(mine.units);
+      x.r.tiles = of(mine.tiles);
+      return cut(x, begin, of(before));
+    }
+    int base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += kBlock) {
+      const int b = b0 + threadIdx.x;
+      int x = 0;
+      if (b < p.B) {
+        const Request r = request_of<kRows, kUnit>(p, off, lengths, b);
+        x = r.units * r.tiles * p.Hkv;
+      }
+#pragma unroll
+      for (int m = 1; m < kWave; m *= 2) {
+        const int o = __shfl_up(x, m);
+        if (lane >= m) x += o;
+      }
+      __syncthreads();
+      if (lane == kWave - 1) carry[wave] = x;
+      __syncthreads();
+      int front = base;
+      for (int i = 0; i < kWaves; ++i) {
+        if (i < wave) front += carry[i];
+        base += carry[i];
+      }
+      if (b < p.B) pre[b + 1] = front + x;
+    }
+    if (threadIdx.x == 0) pre[0] = 0;
+    __syncthreads();
+    runs(uniform(pre[p.B]));
+    return at(begin);
+  }
+
+  __device__ __forceinline__ Piece cut(Piece x, int unit, int start) const {
+    const int rest = unit - start, item = rest / max(1, x.r.units);
+    x.u0 = rest - item * x.r.units;
+    x.u1 = min(x.r.units, x.u0 + (stop - unit));
+    x.g = item / max(1, x.r.tiles);
+    x.rt = item - x.g * x.r.tiles;
+    x.whole = x.u0 == 0 && x.u1 == x.r.units;
+    return x;
+  }
+
+  // The piece that starts at `unit`; pre[] is complete (a barrier lies behind).
+  __device__ __forceinline__ Piece at(int unit) const {
+    Piece x;
+    int b = 0;
+    for (int hi = p.B; hi - b > 1;) {  // the last request that starts at or before it
+      const int mid = (b + hi) / 2;
+      if (pre[mid] <= unit) b = mid;
+      else hi = mid;
+    }
+    x.b = uniform(b);
+    x.r = request_of<kRows, kUnit>(p, off, lengths, x.b);
+    x.r.first = uniform(x.r.first);
+    x.r.n = uniform(x.r.n);
+    x.r.L = uniform(x.r.L);
+    x.r.end = uniform(x.r.end);
+    x.r.units = uniform(x.r.units);
+    x.r.tiles = uniform(x.r.tiles);
+    return cut(x, unit, uniform(pre[x.b]));
+  }
+
+  // What the join has to know of a piece.
+  __device__ __forceinline__ void leave(const Piece& x, int unit) const {
+    if (threadIdx.x != 0) return;
+    const bool last = unit + x.u1 - x.u0 == stop;
+    if (unit == begin && x.u0 == 0) p.split[2 * me].parts = 0;
+    if (last && (x.u0 > 0 || x.whole)) p.split[2 * me + 1].parts = 0;
+    if (x.whole) return;
+    Split s;
+    const int start = unit - x.u0;  // the item's first unit
+    s.k0 = start / share;
+    s.parts = (start + x.r.units - 1) / share - s.k0 + 1;
+    s.at = me - s.k0;
+    s.slot = start == s.k0 * share ? 0 : 1;
+    s.first = x.r.first;
+    s.lines = x.r.n * p.G;
+    s.g = x.g;
+    s.row0 = x.rt * kRows;
+    p.split[2 * me + (x.u0 > 0 ? 0 : 1)] = s;
+  }
+  __device__ __forceinline__ void leave_none() const {
+    if (threadIdx.x < 2) p.split[2 * me + threadIdx.x].parts = 0;
+  }
+};
 
 // kQ groups of 16 rows of a wave: what it knows of them.
 template <class T, int D, int kQ>
@@ -274,7 +341,9 @@ struct Rows {
   }
 
   // Scores without the positions that see[] leaves out.
-  __device__ __forceinline__ static void hide(f32x4 (&s)[kQ][2], const uint32_t (&see)[kQ]) {
+  template <int kN>
+  __device__ __forceinline__ static void hide(f32x4 (&s)[kQ][kN], const uint32_t (&see)[kQ],
+                                              int half) {
     const int quad = here((threadIdx.x & 63) >> 4);
 #pragma unroll
     for (int c = 0; c < kQ; ++c)
@@ -282,18 +351,23 @@ struct Rows {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!(see[c] >> (t * 16 + quad * 4 + i) & 1)) s[c][t][i] = -INFINITY;
+          if (!(see[c] >> (t * 16 + quad * 4 + i) & 1)) s[c][half * 2 + t][i] = -INFINITY;
   }
 
-  // Probabilities of one tile's scores, in the second product's layout:
-  // element e of lane (quad, col) is position e / 4 * 16 + quad * 4 + e % 4.
-  // They are rounded to the cache's type (half a unit in the last place each,
-  // as much as the output's own rounding); the sum takes them unrounded.
-  __device__ __forceinline__ void weigh(const f32x4 (&s)[kQ][2], float scale, uint4 (&pr)[kQ]) {
+  // Probabilities of kN / 2 tiles' scores, in the second product's layout:
+  // element e of lane (quad, col) is position e / 4 * 16 + quad * 4 + e % 4 of
+  // a tile. They are rounded to the cache's type (half a unit in the last
+  // place each, as much as the output's own rounding); the sum takes them
+  // unrounded.
+  template <int kN>
+  __device__ __forceinline__ void weigh(const f32x4 (&s)[kQ][kN], float scale,
+                                        uint4 (&pr)[kN / 2][kQ]) {
 #pragma unroll
     for (int c = 0; c < kQ; ++c) {
-      float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])),
-                       fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < kN; ++t)
+        mx = fmaxf(fmaxf(fmaxf(mx, s[c][t][0]), s[c][t][1]), fmaxf(s[c][t][2], s[c][t][3]));
       mx = max4(mx) * scale;
       // m follows the maximum only when a row has passed it by 2^kLazy.
       if (__any(mx > m[c] + kLazy || (m[c] == -INFINITY && mx > -INFINITY))) {
@@ -304,12 +378,15 @@ struct Rows {
         for (int d = 0; d < kCols; ++d) o[c][d] *= a;
       }
       const float base = m[c] == -INFINITY ? 0.0f : m[c];
-      float e[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        e[i] = __builtin_amdgcn_exp2f(fmaf(s[c][i / 4][i % 4], scale, -base));
-      sum[c] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      pr[c] = pack8<T>(e);
+      for (int h = 0; h < kN / 2; ++h) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          e[i] = __builtin_amdgcn_exp2f(fmaf(s[c][2 * h + i / 4][i % 4], scale, -base));
+        sum[c] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        pr[h][c] = pack8<T>(e);
+      }
     }
   }
 
@@ -376,17 +453,23 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
   constexpr int kPer = kWave / kLanes;  // rows of V per load
   constexpr int kLoads = kTile / kPer;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ int64_t carry[kWaves];
+  __shared__ int carry[kWaves];
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
   uint16_t* const vt = reinterpret_cast<uint16_t*>(smem) + wave * kTile * R::kPitch;
   float2* const ml = reinterpret_cast<float2*>(smem + kWaves * kTile * R::kPitch * 2);
-  int64_t* const pre = reinterpret_cast<int64_t*>(ml + kWaves * kRows);
+  int* const pre = reinterpret_cast<int*>(ml + kWaves * kRows);
 
-  const Run run = deal<kRows, kUnit>(p, off, lengths, pre, carry);
+  Dealer<kRows, kUnit> run(p, off, lengths, pre);
+  Piece x = run.first(carry);
+  if (run.begin >= run.stop) {
+    run.leave_none();
+    return;
+  }
   const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
-  for (int64_t at = run.begin; at < run.stop;) {
-    const Piece x = piece_at<kRows, kUnit>(p, off, lengths, pre, at, run.stop);
+  for (int at = run.begin; at < run.stop;) {
+    if (at != run.begin) x = run.at(at);
+    run.leave(x, at);
     const int32_t* __restrict__ pages = table + (int64_t)x.b * p.max_pages;
     R rows;
     rows.start(p, x, x.rt * kRows);
@@ -503,17 +586,17 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
       if (!inner) {
 #pragma unroll
         for (int c = 0; c < kQ; ++c) see[c] = rows.sees(p, mask, x, c, p0, there);
-        R::hide(s, see);
+        R::hide(s, see, 0);
       }
-      uint4 pr[kQ];
+      uint4 pr[1][kQ];
       rows.weigh(s, p.c, pr);
-      rows.add(vt, pr);
+      rows.add(vt, pr[0]);
       while (odd) {
         const int row = __ffs(odd) - 1;
         odd &= odd - 1;
         const int pg = kPages == 1 ? page_now : __shfl(page_now, row);
-        rows.add_odd(vh + pg * p.page_stride + (int64_t)((p0 + row) & page_mask) * width, row, pr,
-                     see);
+        rows.add_odd(vh + pg * p.page_stride + (int64_t)((p0 + row) & page_mask) * width, row,
+                     pr[0], see);
       }
     }
 
@@ -585,20 +668,26 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
   constexpr int kLanes = D / 8, kPer = kBlock / kLanes;  // rows per load of the block
   constexpr int kLoads = kUnit / kPer;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ int64_t carry[kWaves];
+  __shared__ int carry[kWaves];
   __shared__ uint32_t odd_rows[3][2];  // of the tiles, in turn
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
   // [buffer][K, V][kUnit][kPitch]
   uint16_t* const tiles = reinterpret_cast<uint16_t*>(smem);
   constexpr int kTileElems = kUnit * R::kPitch;
-  int64_t* const pre = reinterpret_cast<int64_t*>(smem + 4 * kTileElems * 2);
+  int* const pre = reinterpret_cast<int*>(smem + 4 * kTileElems * 2);
 
-  const Run run = deal<kRows, kUnit>(p, off, lengths, pre, carry);
+  Dealer<kRows, kUnit> run(p, off, lengths, pre);
+  Piece x = run.first(carry);
+  if (run.begin >= run.stop) {
+    run.leave_none();
+    return;
+  }
   const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
   const int my_row = threadIdx.x / kLanes, my_chunk = threadIdx.x % kLanes;
-  for (int64_t at = run.begin; at < run.stop;) {
-    const Piece x = piece_at<kRows, kUnit>(p, off, lengths, pre, at, run.stop);
+  for (int at = run.begin; at < run.stop;) {
+    if (at != run.begin) x = run.at(at);
+    run.leave(x, at);
     const int32_t* __restrict__ pages = table + (int64_t)x.b * p.max_pages;
     const uint16_t* const kh = p.k + (int64_t)x.g * D;
     const uint16_t* const vh = p.v + (int64_t)x.g * D;
@@ -673,32 +762,36 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
       const bool inner = p0 + kUnit <= x.r.L && __all(page_now >= 0);
       if (busy) {
         const unsigned long long there64 = inner ? ~0ull : __ballot(page_now >= 0);
+        const uint16_t* const kt = tiles + buf * 2 * kTileElems;
+        f32x4 s[kQ][4];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint16_t* const kt = tiles + buf * 2 * kTileElems + half * kTile * R::kPitch;
-          f32x4 s[kQ][2];
+        for (int st = 0; st < R::kSteps; ++st)
 #pragma unroll
-          for (int st = 0; st < R::kSteps; ++st)
+          for (int t = 0; t < 4; ++t) {
+            const uint4 kf = *reinterpret_cast<const uint4*>(kt + (t * 16 + col) * R::kPitch +
+                                                             st * 32 + quad * 8);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              const uint4 kf = *reinterpret_cast<const uint4*>(kt + (t * 16 + col) * R::kPitch +
-                                                               st * 32 + quad * 8);
+            for (int c = 0; c < kQ; ++c)
+              s[c][t] = mfma<T>(kf, rows.q[c][st], st ? s[c][t] : f32x4{0, 0, 0, 0});
+          }
+        uint32_t see[2][kQ];
+        if (!inner) {
 #pragma unroll
-              for (int c = 0; c < kQ; ++c)
-                s[c][t] = mfma<T>(kf, rows.q[c][st], st ? s[c][t] : f32x4{0, 0, 0, 0});
-            }
-          uint32_t see[kQ];
-          if (!inner) {
+          for (int half = 0; half < 2; ++half) {
             const uint32_t there = (uint32_t)(there64 >> (half * 32));
 #pragma unroll
             for (int c = 0; c < kQ; ++c)
-              see[c] = rows.sees(p, mask, x, c, p0 + half * kTile, there);
-            R::hide(s, see);
+              see[half][c] = rows.sees(p, mask, x, c, p0 + half * kTile, there);
+            R::hide(s, see[half], half);
           }
-          uint4 pr[kQ];
-          rows.weigh(s, p.c, pr);
-          rows.add(kt + kTileElems, pr);
-          if (!inner) {
+        }
+        uint4 pr[2][kQ];
+        rows.weigh(s, p.c, pr);
+        rows.add(kt + kTileElems, pr[0]);
+        rows.add(kt + kTileElems + kTile * R::kPitch, pr[1]);
+        if (!inner) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
             uint32_t odd = odd_rows[turn][half];
             while (odd) {
               const int row = __ffs(odd) - 1;
@@ -706,7 +799,7 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
               const int pg = __shfl(page_now, half * kTile + row);
               rows.add_odd(vh + pg * p.page_stride +
                                (int64_t)((p0 + half * kTile + row) & page_mask) * width,
-                           row, pr, see);
+                           row, pr[half], see[half]);
             }
           }
         }
@@ -751,77 +844,110 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
   }
 }
 
-// Joins the parts of the items that several blocks had: a block takes 256 / D
-// rows of an item, its waves every fourth part.
-template <class T, int D, int kRows, int kUnit>
-__global__ __launch_bounds__(kBlock) void join_kernel(const Params p,
-                                                      const int32_t* __restrict__ off,
-                                                      const int32_t* __restrict__ lengths,
-                                                      int max_tiles) {
-  constexpr int kLine = D / 4, kAt = kWave / kLine;  // lanes per row, rows per block
+// Joins the parts of the items that several blocks had. As many blocks join an
+// item as had a part of it, each an equal share of its rows, so that every
+// block reads about as much as it left. A wave takes 256 / D rows at a time:
+// the waves take different rows, kPass at once, or, where a block has few (one
+// long context), every fourth part of the same ones.
+template <class T, int D, int kRows>
+__global__ __launch_bounds__(kBlock) void join_kernel(const Params p) {
+  constexpr int kLine = D / 4, kAt = kWave / kLine;  // lanes per row, rows per wave
+  constexpr int kPass = 4, kU = 8;
   __shared__ f32x4 os[kWaves][kWave];
   __shared__ float2 mls[kWaves][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int i = blockIdx.x;
-  const int rt = i % max_tiles;
-  i /= max_tiles;
-  const int g = i % p.Hkv, b = i / p.Hkv;
-  const int64_t share = p.plan[p.B + 1];
-  const Request r = request_of<kRows, kUnit>(p, off, lengths, b);
-  if (rt >= r.tiles) return;
-  const int64_t a0 = p.plan[b] + ((int64_t)g * r.tiles + rt) * r.units, a1 = a0 + r.units;
-  const int64_t k0 = a0 / share, k1 = (a1 - 1) / share;
-  if (k0 == k1) return;
-  const int row = blockIdx.y * kAt + lane / kLine, ch = lane % kLine;
-  const int line = rt * kRows + row;
-  const bool valid = row < kRows && line < r.n * p.G;
-  f32x4 o = f32x4{0, 0, 0, 0};
-  float m = -INFINITY, sum = 0.0f;
-  if (valid) {
-    constexpr int kU = 4;
-    for (int64_t k = k0 + wave; k <= k1; k += kU * kWaves) {
+  const Split s = p.split[blockIdx.x];
+  if (s.parts == 0) return;
+  const int rows = min(kRows, s.lines - s.row0), ch = lane % kLine;
+  const int each = (rows + s.parts - 1) / s.parts;
+  const int begin = s.at * each, end = min(rows, begin + each);
+  if (begin >= end) return;
+  auto write = [&](int row, f32x4 o, float sum) {
+    const float inv = inverse(sum);
+    const int line = s.row0 + row, nd = line / p.G;
+    *reinterpret_cast<uint2*>(p.out + (int64_t)(s.first + nd) * p.out_stride +
+                              (int64_t)(s.g * p.G + line - nd * p.G) * D + ch * 4) =
+        make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv));
+  };
+  auto part_of = [&](int k, int row) -> int64_t {  // the k-th part's row
+    return (2 * (int64_t)(s.k0 + k) + (k == 0 ? s.slot : 0)) * kRows + row;
+  };
+  if (end - begin > 2 * kAt) {
+    for (int r0 = begin + wave * kPass * kAt; r0 < end; r0 += kWaves * kPass * kAt) {
+      const int row0 = r0 + lane / kLine;
+      f32x4 o[kPass];
+      float m[kPass], sum[kPass];
+#pragma unroll
+      for (int i = 0; i < kPass; ++i) {
+        o[i] = f32x4{0, 0, 0, 0};
+        m[i] = -INFINITY;
+        sum[i] = 0.0f;
+      }
+#pragma unroll 2
+      for (int k = 0; k < s.parts; ++k) {
+        float2 t[kPass];
+        f32x4 x[kPass];
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) {
+          const int64_t at = part_of(k, min(row0 + i * kAt, end - 1));
+          t[i] = p.part_ml[at];
+          x[i] = *reinterpret_cast<const f32x4*>(p.part + at * D + ch * 4);
+        }
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) {
+          const float next = fmaxf(m[i], t[i].x), a = grow(m[i], next), e = grow(t[i].x, next);
+          m[i] = next;
+          sum[i] = sum[i] * a + t[i].y * e;
+          o[i] = o[i] * a + x[i] * e;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kPass; ++i)
+        if (row0 + i * kAt < end) write(row0 + i * kAt, o[i], sum[i]);
+    }
+    return;
+  }
+  for (int r0 = begin; r0 < end; r0 += kAt) {
+    const int row = min(r0 + lane / kLine, end - 1);
+    f32x4 o = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, sum = 0.0f;
+    for (int k = wave; k < s.parts; k += kU * kWaves) {
       float2 t[kU];
       f32x4 x[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
-        const int64_t kk = k + u * kWaves;
-        if (kk <= k1) {
-          const int64_t at = (2 * kk + (kk == k0 && a0 != k0 * share ? 1 : 0)) * kRows + row;
-          t[u] = p.part_ml[at];
-          x[u] = *reinterpret_cast<const f32x4*>(p.part + at * D + ch * 4);
-        } else {
-          t[u] = make_float2(-INFINITY, 0.0f);
-          x[u] = f32x4{0, 0, 0, 0};
-        }
+        const int64_t at = part_of(min(k + u * kWaves, s.parts - 1), row);
+        t[u] = p.part_ml[at];
+        x[u] = *reinterpret_cast<const f32x4*>(p.part + at * D + ch * 4);
       }
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
+        if (k + u * kWaves >= s.parts) break;
         const float next = fmaxf(m, t[u].x), a = grow(m, next), e = grow(t[u].x, next);
         m = next;
         sum = sum * a + t[u].y * e;
         o = o * a + x[u] * e;
       }
     }
-  }
-  os[wave][lane] = o;
-  mls[wave][lane] = make_float2(m, sum);
-  __syncthreads();
-  if (wave != 0 || !valid) return;
-  float top = -INFINITY, whole = 0.0f;
+    os[wave][lane] = o;
+    mls[wave][lane] = make_float2(m, sum);
+    __syncthreads();
+    if (wave == 0 && r0 + lane / kLine < end) {
+      float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mls[w][lane].x);
-  f32x4 x = f32x4{0, 0, 0, 0};
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mls[w][lane].x);
+      sum = 0.0f;
+      o = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float a = grow(mls[w][lane].x, top);
-    whole += mls[w][lane].y * a;
-    x += os[w][lane] * a;
+      for (int w = 0; w < kWaves; ++w) {
+        const float a = grow(mls[w][lane].x, top);
+        sum += mls[w][lane].y * a;
+        o += os[w][lane] * a;
+      }
+      write(row, o, sum);
+    }
+    __syncthreads();
   }
-  const float inv = inverse(whole);
-  const int nd = line / p.G;
-  *reinterpret_cast<uint2*>(p.out + (int64_t)(r.first + nd) * p.out_stride +
-                            (int64_t)(g * p.G + line - nd * p.G) * D + ch * 4) =
-      make_uint2(T::pack(x[0] * inv, x[1] * inv), T::pack(x[2] * inv, x[3] * inv));
 }
 
 // Which kernel: rows of one KV head at most, over 16-row groups.
@@ -846,16 +972,16 @@ constexpr int occupancy(int D, int q, bool shared) {
 constexpr int rows_of(Shape s) { return 16 * s.q * (s.shared ? kWaves : 1); }
 
 struct Layout {
-  size_t plan, part_ml, part, bytes;
+  size_t part_ml, part, bytes;
 };
 
 Layout layout(const tg_tree_attn_args* a) {
   const Shape sh = shape_of(a);
   const int D = a->cache.D;
-  const size_t slots = 2 * (size_t)kCus * occupancy(D, sh.q, sh.shared) * rows_of(sh);
+  const size_t blocks = (size_t)kCus * occupancy(D, sh.q, sh.shared);
+  const size_t slots = 2 * blocks * rows_of(sh);
   Layout L;
-  L.plan = 0;
-  L.part_ml = ((size_t)(a->cache.B + 2) * 8 + 255) & ~(size_t)255;
+  L.part_ml = (2 * blocks * sizeof(Split) + 255) & ~(size_t)255;
   L.part = L.part_ml + slots * 8;
   L.bytes = L.part + slots * D * 4;
   return L;
@@ -878,7 +1004,7 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
   p.out_stride = a->out_stride;
   p.page_stride = c.page_stride;
   p.out = static_cast<uint16_t*>(a->out);
-  p.plan = reinterpret_cast<int64_t*>(w + L.plan);
+  p.split = reinterpret_cast<Split*>(w);
   p.part_ml = reinterpret_cast<float2*>(w + L.part_ml);
   p.part = reinterpret_cast<float*>(w + L.part);
   p.page_shift = __builtin_ctz(c.page_size);
@@ -902,7 +1028,7 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
                        a->q_offsets, a->lengths, a->tree_mask);
     return hipGetLastError();
   };
-  const size_t pre = (size_t)(c.B + 1) * 8;
+  const size_t pre = (size_t)(c.B + 1) * 4;
   hipError_t e;
   if constexpr (kShared) {
     e = go(shared_kernel<T, D, kQ, kOcc>, (size_t)4 * kUnit * kPitch * 2 + pre);
@@ -913,11 +1039,7 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
                                    : go(split_kernel<T, D, kQ, 0, kOcc>, lds);
   }
   if (e != hipSuccess) return e;
-  const int rows = a->max_nodes * p.G, tiles = (rows + kRows - 1) / kRows;
-  const int line = rows < kRows ? rows : kRows, at = 256 / D;
-  hipLaunchKernelGGL((join_kernel<T, D, kRows, kUnit>),
-                     dim3(c.B * c.Hkv * tiles, (line + at - 1) / at), dim3(kBlock), 0, s, p,
-                     a->q_offsets, a->lengths, tiles);
+  hipLaunchKernelGGL((join_kernel<T, D, kRows>), dim3(2 * kCus * kOcc), dim3(kBlock), 0, s, p);
   return hipGetLastError();
 }
 
