@@ -78,15 +78,21 @@ __device__ __forceinline__ int here(int x) {
   return x;
 }
 
+// The larger one, NaN if either is (one instruction for three values; fmaxf
+// costs another per value that comes out of a matrix product).
+__device__ __forceinline__ float most(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+
 // Over the four lanes that share a row of S (they differ in lane / 16).
 // The swaps give each lane its own half's (row's) values and the other's.
 __device__ __forceinline__ float max4(float x) {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   const uint32_t u = __float_as_uint(x);
   const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(u, u, false, false));
-  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const uint32_t v = __float_as_uint(most(__uint_as_float(a[0]), __uint_as_float(a[1])));
   const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  return most(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum4(float x) {
   x += __shfl_xor(x, 16);
@@ -367,7 +373,7 @@ struct Rows {
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < kN; ++t)
-        mx = fmaxf(fmaxf(fmaxf(mx, s[c][t][0]), s[c][t][1]), fmaxf(s[c][t][2], s[c][t][3]));
+        mx = most(most(most(mx, s[c][t][0]), s[c][t][1]), most(s[c][t][2], s[c][t][3]));
       mx = max4(mx) * scale;
       // m follows the maximum only when a row has passed it by 2^kLazy.
       if (__any(mx > m[c] + kLazy || (m[c] == -INFINITY && mx > -INFINITY))) {
@@ -659,7 +665,9 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
 // The four waves take kQ groups of 16 rows each and share tiles of 64
 // positions, which go from registers into one of two LDS buffers while the
 // other is multiplied.
-template <class T, int D, int kQ, int kOcc>
+// kEven: a page holds the rows that a wave loads at once, whose address is the
+// wave's then.
+template <class T, int D, int kQ, bool kEven, int kOcc>
 __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     const Params p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
     const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
@@ -685,6 +693,7 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
   }
   const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
   const int my_row = threadIdx.x / kLanes, my_chunk = threadIdx.x % kLanes;
+  const uint32_t my_at = (lane / kLanes * width + my_chunk * 8) * 2;
   for (int at = run.begin; at < run.stop;) {
     if (at != run.begin) x = run.at(at);
     run.leave(x, at);
@@ -706,11 +715,20 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     auto load_tile = [&](int p0, int page) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
-        const int row = j * kPer + my_row, pg = __shfl(page, row);
-        const int64_t from = (pg < 0 ? 0 : pg * p.page_stride +
-                              (int64_t)((p0 + row) & page_mask) * width) + my_chunk * 8;
-        kn[j] = *reinterpret_cast<const u32x4*>(kh + from);
-        vn[j] = *reinterpret_cast<const u32x4*>(vh + from);
+        if (kEven) {
+          const int row = j * kPer + wave * (kWave / kLanes);
+          const int64_t from =
+              (int64_t)max(__builtin_amdgcn_readlane(page, row), 0) * p.page_stride +
+              (int64_t)((p0 + row) & page_mask) * width;
+          kn[j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(kh + from) + my_at);
+          vn[j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(vh + from) + my_at);
+        } else {
+          const int row = j * kPer + my_row, pg = __shfl(page, row);
+          const int64_t from = (pg < 0 ? 0 : pg * p.page_stride +
+                                (int64_t)((p0 + row) & page_mask) * width) + my_chunk * 8;
+          kn[j] = *reinterpret_cast<const u32x4*>(kh + from);
+          vn[j] = *reinterpret_cast<const u32x4*>(vh + from);
+        }
       }
     };
     // The loaded tile into buffer `buf`; rows of V that are not there are 0,
@@ -1031,7 +1049,9 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
   const size_t pre = (size_t)(c.B + 1) * 4;
   hipError_t e;
   if constexpr (kShared) {
-    e = go(shared_kernel<T, D, kQ, kOcc>, (size_t)4 * kUnit * kPitch * 2 + pre);
+    const size_t lds = (size_t)4 * kUnit * kPitch * 2 + pre;
+    e = c.page_size >= 512 / D ? go(shared_kernel<T, D, kQ, true, kOcc>, lds)
+                               : go(shared_kernel<T, D, kQ, false, kOcc>, lds);
   } else {
     const size_t lds = (size_t)kWaves * kTile * kPitch * 2 + kWaves * kRows * 8 + pre;
     e = c.page_size >= kTile   ? go(split_kernel<T, D, kQ, 1, kOcc>, lds)
