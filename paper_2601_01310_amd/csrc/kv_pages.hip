@@ -179,6 +179,7 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(
   const bool fits = good && (need == 0 || sum <= got);
   if (i < n) {
     status[i] = fits;
+    if (!fits) len[i] = 0;  // nothing is shared
     if (fits) {
       const int whole = len[i] >> page_shift;
       if (need) {
@@ -193,7 +194,6 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(
   __syncthreads();
   // Whole pages are shared: a wave takes a fork.
   for (int f = threadIdx.x / kWave; f < n; f += kWaves) {
-    if (!status[f]) continue;
     const int32_t* s = table + (long)from[f] * max_pages;
     int32_t* d = table + (long)to[f] * max_pages;
     for (int j = threadIdx.x % kWave; j < len[f] >> page_shift; j += kWave) {
@@ -210,18 +210,18 @@ __global__ __launch_bounds__(256) void fork_copy_kernel(
     const int32_t* __restrict__ lengths, const int32_t* __restrict__ src,
     const int32_t* __restrict__ dst, const int32_t* __restrict__ status, uint16_t* k, uint16_t* v,
     int64_t layer_stride, int64_t page_stride, int row) {
-  const int f = blockIdx.x;
-  if (!status[f]) return;
-  const int d = dst[f], L = lengths[d], rows = L & ((1 << page_shift) - 1);
+  const int f = blockIdx.x, done = status[f], from = src[f], d = dst[f];
+  if (!done) return;
+  const int L = lengths[d], rows = L & ((1 << page_shift) - 1);
   if (rows == 0) return;
   const int whole = L >> page_shift;
-  const int ps = table[(long)src[f] * max_pages + whole], pd = table[(long)d * max_pages + whole];
+  const int ps = table[(long)from * max_pages + whole], pd = table[(long)d * max_pages + whole];
   if (ps < 0 || ps >= n_pages || pd < 0 || pd >= n_pages) return;
   uint16_t* base = (blockIdx.y & 1 ? v : k) + (int64_t)(blockIdx.y >> 1) * layer_stride;
   const uint4* s = reinterpret_cast<const uint4*>(base + ps * page_stride);
   uint4* o = reinterpret_cast<uint4*>(base + pd * page_stride);
   const int chunks = rows * (row / 8);
-  constexpr int kU = 4;
+  constexpr int kU = 8;
   for (int c0 = blockIdx.z * 256 * kU + threadIdx.x; c0 < chunks; c0 += gridDim.z * 256 * kU) {
     uint4 x[kU];
 #pragma unroll
@@ -250,18 +250,7 @@ __global__ __launch_bounds__(256) void trim_kernel(int32_t* table, int32_t* held
   if (threadIdx.x == 0) held[b] = (int)pages;
 }
 
-// Position -> element offset of its row in a layer, or -1.
-__device__ __forceinline__ int64_t row_at(const int32_t* __restrict__ row, int64_t pos, int n_pages,
-                                          int page_shift, int max_pages, int64_t page_stride,
-                                          int width) {
-  const int64_t j = pos >> page_shift;
-  if (pos < 0 || j >= max_pages) return -1;
-  const int p = row[j];
-  if (p < 0 || p >= n_pages) return -1;
-  return p * page_stride + (pos & ((1 << page_shift) - 1)) * width;
-}
-
-// One block per request, layer and K or V; a thread takes a 16-byte column
+// One block per request and layer; a thread takes a 16-byte column of K or V
 // through the kept rows. Rows move down (path[i] >= i, ascending), so a batch
 // of rows is read before any of them is written and later rows are still
 // whole.
@@ -270,33 +259,48 @@ __global__ __launch_bounds__(256) void compact_kernel(
     const int32_t* __restrict__ path, int max_path, const int32_t* __restrict__ n_keep,
     const int32_t* __restrict__ lengths, int32_t* __restrict__ new_lengths, uint16_t* k, uint16_t* v,
     int64_t layer_stride, int64_t page_stride, int width) {
-  const int b = blockIdx.x, L = max(0, lengths[b]);
+  // A table reaches at most 2^30 positions.
+  const int b = blockIdx.x, L = max(0, min(lengths[b], 1 << 30));
   const int n = max(0, min(n_keep[b], max_path));
-  if (blockIdx.y == 0 && threadIdx.x == 0) new_lengths[b] = L + n;
-  uint16_t* base = (blockIdx.y & 1 ? v : k) + (int64_t)(blockIdx.y >> 1) * layer_stride;
+  if (blockIdx.y == 0 && threadIdx.x == 0) new_lengths[b] = max(0, lengths[b]) + n;
   const int32_t* row = table + (long)b * max_pages;
   path += (long)b * max_path;
   constexpr int kU = 8;
-  for (int c = threadIdx.x * 8; c < width; c += 256 * 8) {
-    for (int i0 = 0; i0 < n; i0 += kU) {
-      uint4 x[kU];
-      int64_t to[kU];
+  const int in_page = (1 << page_shift) - 1;
+  // Logical page of a position that the table reaches, -1 for others.
+  auto page_of = [&](int pos) { return pos >> page_shift < max_pages ? pos >> page_shift : -1; };
+  for (int i0 = 0; i0 < n; i0 += kU) {
+    // The batch's places, each kind of load together: one after another they
+    // cost a memory latency per row and kind.
+    int j[kU], from[kU], at[kU];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int i = i0 + u, j = i < n ? path[i] : -1;
-        to[u] = -1;
-        if (j <= i) continue;  // in its place already (or no place at all)
-        const int64_t from =
-            row_at(row, (int64_t)L + j, n_pages, page_shift, max_pages, page_stride, width);
-        const int64_t at =
-            row_at(row, (int64_t)L + i, n_pages, page_shift, max_pages, page_stride, width);
-        if (from < 0 || at < 0) continue;
-        to[u] = at;
-        x[u] = *reinterpret_cast<const uint4*>(base + from + c);
-      }
+    for (int u = 0; u < kU; ++u) j[u] = path[min(i0 + u, n - 1)];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = i0 + u;
+      // In its place already, or no place at all: not moved.
+      const bool moves = i < n && j[u] > i && j[u] < (1 << 30);
+      const int pf = moves ? page_of(L + j[u]) : -1, pt = moves ? page_of(L + i) : -1;
+      from[u] = pf < 0 ? -1 : row[pf];
+      at[u] = pt < 0 ? -1 : row[pt];
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (from[u] >= n_pages || at[u] >= n_pages || at[u] < 0) from[u] = -1;
+    for (int c = threadIdx.x * 8; c < 2 * width; c += 256 * 8) {
+      uint16_t* const base =
+          (c < width ? k : v - width) + (int64_t)blockIdx.y * layer_stride + c;
+      uint4 x[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u)
-        if (to[u] >= 0) *reinterpret_cast<uint4*>(base + to[u] + c) = x[u];
+        if (from[u] >= 0)
+          x[u] = *reinterpret_cast<const uint4*>(base + from[u] * page_stride +
+                                                 (int64_t)((L + j[u]) & in_page) * width);
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        if (from[u] >= 0)
+          *reinterpret_cast<uint4*>(base + at[u] * page_stride +
+                                    (int64_t)((L + i0 + u) & in_page) * width) = x[u];
     }
   }
 }
@@ -307,7 +311,7 @@ hipError_t launch_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_
                              const int32_t* n_keep, const int32_t* lengths, int32_t* new_lengths,
                              hipStream_t s) {
   if (c->B == 0) return hipSuccess;
-  hipLaunchKernelGGL(compact_kernel, dim3(c->B, 2 * c->n_layers), dim3(256), 0, s, c->page_table,
+  hipLaunchKernelGGL(compact_kernel, dim3(c->B, c->n_layers), dim3(256), 0, s, c->page_table,
                      c->n_pages, __builtin_ctz(c->page_size), c->max_pages, path, max_path, n_keep,
                      lengths, new_lengths, static_cast<uint16_t*>(c->k),
                      static_cast<uint16_t*>(c->v), c->layer_stride, c->page_stride, c->Hkv * c->D);

@@ -58,6 +58,29 @@ def _rows(t: torch.Tensor, name: str, dtype, inner) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(dense, t.stride(0))
 
 
+def _stream(stream, device: int) -> int:
+    """Raw handle of ``stream``, or of the current one of the tensors' device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _check(status: int, where: str):
+    if status != tg.TG_OK:
+        raise tg.TgError(status, where)
+
+
+def _int32(t: torch.Tensor, name: str, device: int, n: int, dim: int = 1) -> int:
+    """Address of a dense int32 tensor on ``device`` with n elements (-1: any),
+    checked in a few short calls: the page calls are a microsecond's work on
+    the host otherwise."""
+    if (t.dtype is torch.int32 and t.get_device() == device and t.dim() == dim
+            and (n < 0 or t.numel() == n) and t.is_contiguous()):
+        return t.data_ptr()
+    _want(t, name, torch.int32, (None if n < 0 else n,) if dim == 1 else (None,) * dim)
+    raise ValueError(f"{name} is {list(t.shape)} on {t.device}: not what the cache needs")
+
+
 def _same_device(*tensors):
     devices = {t.device for t in tensors if t is not None}
     if len(devices) > 1:
@@ -96,6 +119,7 @@ class KvCache:
         a.page_stride = k.stride(1) if pages > 1 else size * Hkv * D
         a.k, a.v, a.page_table = k.data_ptr(), v.data_ptr(), page_table.data_ptr()
         a.held, a.refcount = held.data_ptr(), refcount.data_ptr()
+        self._ref, self._device = ctypes.byref(a), k.get_device()
 
     @classmethod
     def empty(cls, n_layers, n_pages, page_size, Hkv, D, B, max_pages, dtype=torch.bfloat16,
@@ -109,38 +133,34 @@ class KvCache:
 
     def reserve(self, lengths, q_offsets, slots, status, stream=None):
         """Pages for the new rows; fills ``slots`` [T] and ``status`` [B]."""
-        B = self.args.B
-        _want(lengths, "lengths", torch.int32, (B,))
-        _want(q_offsets, "q_offsets", torch.int32, (B + 1,))
-        _want(slots, "slots", torch.int32, (None,))
-        _want(status, "status", torch.int32, (B,))
-        _same_device(self.k, lengths, q_offsets, slots, status)
-        tg.tg_kv_pages_reserve(self.args, lengths, q_offsets, slots.shape[0], slots, status, stream)
+        B, d = self.args.B, self._device
+        _check(tg.load().tg_kv_pages_reserve(
+            self._ref, _int32(lengths, "lengths", d, B), _int32(q_offsets, "q_offsets", d, B + 1),
+            slots.shape[0], _int32(slots, "slots", d, -1), _int32(status, "status", d, B),
+            _stream(stream, d)), "tg_kv_pages_reserve")
 
     def fork(self, lengths, src, dst, status, stream=None):
         """Requests ``dst`` become copies of ``src``; updates ``lengths``."""
-        _want(lengths, "lengths", torch.int32, (self.args.B,))
-        _want(src, "src", torch.int32, (None,))
-        _want(dst, "dst", torch.int32, (src.shape[0],))
-        _want(status, "status", torch.int32, (src.shape[0],))
-        _same_device(self.k, lengths, src, dst, status)
-        tg.tg_kv_pages_fork(self.args, lengths, src, dst, src.shape[0], status, stream)
+        n, d = src.shape[0], self._device
+        _check(tg.load().tg_kv_pages_fork(
+            self._ref, _int32(lengths, "lengths", d, self.args.B), _int32(src, "src", d, n),
+            _int32(dst, "dst", d, n), n, _int32(status, "status", d, n), _stream(stream, d)),
+            "tg_kv_pages_fork")
 
     def trim(self, keep, stream=None):
         """Gives back the pages past ``keep`` [B] tokens of each request."""
-        _want(keep, "keep", torch.int32, (self.args.B,))
-        _same_device(self.k, keep)
-        tg.tg_kv_pages_trim(self.args, keep, stream)
+        _check(tg.load().tg_kv_pages_trim(
+            self._ref, _int32(keep, "keep", self._device, self.args.B),
+            _stream(stream, self._device)), "tg_kv_pages_trim")
 
     def compact(self, path, n_keep, lengths, new_lengths, stream=None):
         """Moves the kept rows of every layer together (``path`` [B, max_path]
         and ``n_keep`` [B] as :class:`VerifyTree` returns them)."""
-        B = self.args.B
-        _want(path, "path", torch.int32, (B, None))
-        for name, t in (("n_keep", n_keep), ("lengths", lengths), ("new_lengths", new_lengths)):
-            _want(t, name, torch.int32, (B,))
-        _same_device(self.k, path, n_keep, lengths, new_lengths)
-        tg.tg_kv_compact(self.args, path, path.shape[1], n_keep, lengths, new_lengths, stream)
+        B, d, most = self.args.B, self._device, path.shape[-1]
+        _check(tg.load().tg_kv_compact(
+            self._ref, _int32(path, "path", d, B * most, 2), most, _int32(n_keep, "n_keep", d, B),
+            _int32(lengths, "lengths", d, B), _int32(new_lengths, "new_lengths", d, B),
+            _stream(stream, d)), "tg_kv_compact")
 
 
 class QkNormRope:
@@ -177,9 +197,12 @@ class QkNormRope:
                             positions=positions, slots=slots, q_out=q_out).items():
             setattr(a, name, None if t is None else t.data_ptr())
 
+        self._ref, self._device = ctypes.byref(a), qkv.get_device()
+
     def __call__(self, layer=0, stream=None):
         self.args.layer = layer
-        tg.tg_qk_norm_rope(self.args, stream)
+        _check(tg.load().tg_qk_norm_rope(self._ref, _stream(stream, self._device)),
+               "tg_qk_norm_rope")
         return self.q_out
 
 
@@ -227,10 +250,12 @@ class TreeAttention:
             raise tg.TgError(tg.load().tg_tree_attention(ctypes.byref(a), None, 0, None),
                              "workspace")
         self.ws = tg.workspace(self.ws_bytes, q.device)
+        self._ref, self._device, self._ws = ctypes.byref(a), q.get_device(), self.ws.data_ptr()
 
     def __call__(self, layer=0, stream=None):
         self.args.layer = layer
-        tg.tg_tree_attention(self.args, self.ws, self.ws_bytes, stream)
+        _check(tg.load().tg_tree_attention(self._ref, self._ws, self.ws_bytes,
+                                           _stream(stream, self._device)), "tg_tree_attention")
         return self.out
 
 
@@ -276,7 +301,10 @@ class VerifyTree:
         if self.ws_bytes == 0:
             raise tg.TgError(tg.load().tg_verify_tree(ctypes.byref(a), None, 0, None), "workspace")
         self.ws = tg.workspace(self.ws_bytes, target_probs.device)
+        self._ref, self._device = ctypes.byref(a), target_probs.get_device()
+        self._ws = self.ws.data_ptr()
 
     def __call__(self, stream=None):
-        tg.tg_verify_tree(self.args, self.ws, self.ws_bytes, stream)
+        _check(tg.load().tg_verify_tree(self._ref, self._ws, self.ws_bytes,
+                                        _stream(stream, self._device)), "tg_verify_tree")
         return self.tokens_out, self.path, self.n_out
