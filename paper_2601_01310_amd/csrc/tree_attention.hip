@@ -977,6 +977,7 @@ struct Shape {
 Shape shape_of(const tg_tree_attn_args* a) {
   const int rows = a->max_nodes * (a->Hq / a->cache.Hkv);
   if (rows <= 16) return {1, false};
+  if (a->cache.D == 256) return {1, true};
   if (rows <= 32) return {2, false};
   if (rows <= 64) return {1, true};
   return {2, true};
@@ -984,7 +985,7 @@ Shape shape_of(const tg_tree_attn_args* a) {
 
 // Waves per SIMD that the registers leave.
 constexpr int occupancy(int D, int q, bool shared) {
-  return D == 64 ? (q == 2 ? 2 : 3) : D == 128 ? 2 : q == 1 ? 2 : 1;
+  return D == 64 ? (q == 2 ? 2 : 3) : D == 128 ? 2 : 1;
 }
 
 constexpr int rows_of(Shape s) { return 16 * s.q * (s.shared ? kWaves : 1); }
@@ -1066,8 +1067,10 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
 template <class T, int D>
 hipError_t launch_shape(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
   const Shape sh = shape_of(a);
-  if (sh.shared) return sh.q == 1 ? launch<T, D, 1, true>(a, ws, s) : launch<T, D, 2, true>(a, ws, s);
-  return sh.q == 1 ? launch<T, D, 1, false>(a, ws, s) : launch<T, D, 2, false>(a, ws, s);
+  if (sh.q == 1) return sh.shared ? launch<T, D, 1, true>(a, ws, s) : launch<T, D, 1, false>(a, ws, s);
+  if constexpr (D < 256)
+    return sh.shared ? launch<T, D, 2, true>(a, ws, s) : launch<T, D, 2, false>(a, ws, s);
+  return hipErrorInvalidValue;  // shape_of() gives no other
 }
 
 template <class T>
