@@ -71,6 +71,13 @@ __device__ __forceinline__ uint32_t odd_part(uint32_t u, bool keep) {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// load_lds16() from an address per lane. (The compiler waits for these before
+// any later LDS read; for those of load_lds16() it leaves the wait to us.)
+__device__ __forceinline__ void load_lds(const uint16_t* from, lds_u16* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
 // x, of which the compiler knows nothing: what is computed from it stays where
 // it is and takes no registers outside (rare paths inside the main loop).
 __device__ __forceinline__ int here(int x) {
@@ -346,6 +353,27 @@ struct Rows {
     return there & (ctx ? own << ctx | ((1u << ctx) - 1) : own);
   }
 
+  // Scores of a tile of 64 positions in LDS, rows D apart: `kt` is the lane's
+  // row of the first 16, `chunk` its chunk of the first step. `apart`, here and
+  // below, is only named: reads beside a restricted pointer are ones for which
+  // the compiler does not wait for loads on their way into LDS (into the other
+  // buffer; a barrier lies between these and this tile's).
+  __device__ __forceinline__ void scores(const uint16_t* kt, int chunk, f32x4 (&s)[kQ][4],
+                                         const uint16_t* __restrict__ apart) const {
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const u32x4 raw =
+            *reinterpret_cast<const u32x4*>(kt + t * 16 * D + (chunk ^ (st * 4)) * 8);
+        const uint4 kf = __builtin_bit_cast(uint4, raw);
+#pragma unroll
+        for (int c = 0; c < kQ; ++c)
+          s[c][t] = mfma<T>(kf, q[c][st], st ? s[c][t] : f32x4{0, 0, 0, 0});
+      }
+    asm volatile("" ::"s"(apart));
+  }
+
   // Scores without the positions that see[] leaves out.
   template <int kN>
   __device__ __forceinline__ static void hide(f32x4 (&s)[kQ][kN], const uint32_t (&see)[kQ],
@@ -396,19 +424,18 @@ struct Rows {
     }
   }
 
-  // o += V^T P^T over the 32 rows of V at vt (LDS, kPitch apart).
-  __device__ __forceinline__ void add(const uint16_t* vt, const uint4 (&pr)[kQ]) {
-    const int col = threadIdx.x & 15, quad = (threadIdx.x & 63) >> 4;
-    // A lane reads 4 columns of row quad * 4 + col / 4 (and of the row 16
-    // below) and gets column `col` of the rows quad * 4 .. + 3.
-    const uint16_t* src = vt + (quad * 4 + col / 4) * kPitch + (col & 3) * 4;
+  // o += V^T P^T over 32 rows of V in LDS; at(h, d): where the lane reads 4
+  // columns, from 16 d on, of row quad * 4 + col / 4 of half h (it gets column
+  // `col` of the rows quad * 4 .. + 3).
+  template <class At>
+  __device__ __forceinline__ void add(At at, const uint4 (&pr)[kQ],
+                                      const uint16_t* __restrict__ apart) {
 #pragma unroll
     for (int d = 0; d < kCols; ++d) {
       s16x8 a;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(src + h * 16 * kPitch + d * 16));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at(h, d));
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[h * 4 + i] = x[i];
       }
@@ -416,6 +443,7 @@ struct Rows {
 #pragma unroll
       for (int c = 0; c < kQ; ++c) o[c][d] = mfma<T>(va, pr[c], o[c][d]);
     }
+    asm volatile("" ::"s"(apart));
   }
 
   // The infinities and NaN of row `row` (0 .. 31) of the tile, which the tile
@@ -480,12 +508,16 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
     R rows;
     rows.start(p, x, x.rt * kRows);
 
-    // Page of position p0 + lane % 32 (kPages == 1: of the tile), -1 for none.
-    auto page_at = [&](int p0) -> int {
+    // The table's entry for position p0 + lane % 32 (kPages == 1: of the tile),
+    // and the page that it is, -1 for none: looked at only where it is used,
+    // since waiting for it means waiting for all loads before it.
+    auto entry_at = [&](int p0) -> int {
       const int pos = kPages == 1 ? p0 : p0 + (lane & 31);
-      if (pos >= x.r.end) return -1;
-      const int g0 = pages[pos >> p.page_shift];
-      return g0 >= 0 && g0 < p.n_pages ? g0 : -1;
+      return pages[min(pos, x.r.end - 1) >> p.page_shift];
+    };
+    auto page_of = [&](int entry, int p0) -> int {
+      const int pos = kPages == 1 ? p0 : p0 + (lane & 31);
+      return pos < x.r.end && entry >= 0 && entry < p.n_pages ? entry : -1;
     };
     uint4 kn[2][R::kSteps], vn[kLoads];
     // Loads of the tile at p0; positions without a page read page 0 and are
@@ -533,9 +565,9 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
 
     int p0 = (x.u0 * kWaves + wave) * kTile;
     const int p_end = min(x.r.end, x.u1 * kUnit);
-    int page = page_at(p0);
+    int page = page_of(entry_at(p0), p0);
     if (p0 < p_end) load_tile(p0, page);
-    int page_next = page_at(p0 + kUnit);
+    int entry = entry_at(p0 + kUnit);
     for (; p0 < p_end; p0 += kUnit) {
       const bool inner = p0 + kTile <= x.r.L && __all(page >= 0);
       uint32_t there = ~0u;  // positions of the tile that are there at all
@@ -581,10 +613,10 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
       // The next loads take the place of this tile's operands: not before.
       __builtin_amdgcn_sched_barrier(0);
       const int page_now = page;
-      page = page_next;
       if (p0 + kUnit < p_end) {
+        page = page_of(entry, p0 + kUnit);
         load_tile(p0 + kUnit, page);
-        page_next = page_at(p0 + 2 * kUnit);
+        entry = entry_at(p0 + 2 * kUnit);
       }
 
       __builtin_amdgcn_sched_barrier(0);
@@ -596,7 +628,8 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
       }
       uint4 pr[1][kQ];
       rows.weigh(s, p.c, pr);
-      rows.add(vt, pr[0]);
+      const uint16_t* const vr = vt + (quad * 4 + col / 4) * R::kPitch + (col & 3) * 4;
+      rows.add([&](int h, int d) { return vr + h * 16 * R::kPitch + d * 16; }, pr[0], vh);
       while (odd) {
         const int row = __ffs(odd) - 1;
         odd &= odd - 1;
@@ -663,8 +696,11 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
 }
 
 // The four waves take kQ groups of 16 rows each and share tiles of 64
-// positions, which go from registers into one of two LDS buffers while the
-// other is multiplied.
+// positions, which go straight from the cache into one of two LDS buffers
+// (no registers, no LDS instructions) while the other is multiplied. A row of
+// a tile is D / 8 chunks of 16 bytes, chunk c at place c ^ turn(row): the
+// transposing reads of four rows and the operand reads of eight hit different
+// banks, as rows of other lengths would do, which these loads cannot write.
 // kEven: a page holds the rows that a wave loads at once, whose address is the
 // wave's then.
 template <class T, int D, int kQ, bool kEven, int kOcc>
@@ -673,17 +709,18 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
   using R = Rows<T, D, kQ>;
   constexpr int kRows = 16 * kQ * kWaves, kUnit = 2 * kTile;
-  constexpr int kLanes = D / 8, kPer = kBlock / kLanes;  // rows per load of the block
-  constexpr int kLoads = kUnit / kPer;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int kLanes = D / 8;            // lanes per row
+  constexpr int kHave = kWave / kLanes;    // rows per load of a wave
+  constexpr int kLoads = kUnit / (kHave * kWaves);
+  constexpr int kTileElems = kUnit * D;
+  // [buffer][K, V][kUnit][D]
+  __shared__ __attribute__((aligned(16))) uint16_t tiles[4 * kTileElems];
+  extern __shared__ __attribute__((aligned(16))) int pre[];
   __shared__ int carry[kWaves];
   __shared__ uint32_t odd_rows[3][2];  // of the tiles, in turn
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
-  // [buffer][K, V][kUnit][kPitch]
-  uint16_t* const tiles = reinterpret_cast<uint16_t*>(smem);
-  constexpr int kTileElems = kUnit * R::kPitch;
-  int* const pre = reinterpret_cast<int*>(smem + 4 * kTileElems * 2);
+  auto turn_of = [](int row) { return (D == 64 ? row >> 1 & 3 : row & 7) * 2; };
 
   Dealer<kRows, kUnit> run(p, off, lengths, pre);
   Piece x = run.first(carry);
@@ -692,8 +729,14 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     return;
   }
   const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
-  const int my_row = threadIdx.x / kLanes, my_chunk = threadIdx.x % kLanes;
+  // The lane's row and chunk in a wave's load (load j: rows j * kHave * kWaves
+  // on; a multiple of 8 rows, so that the chunk is the same in all of them).
+  const int my_row = wave * kHave + lane / kLanes;
+  const int my_chunk = lane % kLanes ^ turn_of(my_row);
   const uint32_t my_at = (lane / kLanes * width + my_chunk * 8) * 2;
+  // Where the lane reads K (first step) and V (first columns) of a tile.
+  const int k_chunk = quad ^ turn_of(col), v_row = quad * 4 + col / 4;
+  const int v_chunk = (col & 3) / 2 ^ turn_of(v_row);
   for (int at = run.begin; at < run.stop;) {
     if (at != run.begin) x = run.at(at);
     run.leave(x, at);
@@ -705,93 +748,84 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     R rows;
     rows.start(p, x, row0);
 
-    // Page of position p0 + lane, -1 for none.
-    auto page_at = [&](int p0) -> int {
-      if (p0 + lane >= x.r.end) return -1;
-      const int g0 = pages[(p0 + lane) >> p.page_shift];
-      return g0 >= 0 && g0 < p.n_pages ? g0 : -1;
+    // The table's entry for position p0 + lane and the page that it is, as above.
+    auto entry_at = [&](int p0) -> int {
+      return pages[min(p0 + lane, x.r.end - 1) >> p.page_shift];
     };
-    u32x4 kn[kLoads], vn[kLoads];
-    auto load_tile = [&](int p0, int page) {
+    auto page_of = [&](int entry, int p0) -> int {
+      return p0 + lane < x.r.end && entry >= 0 && entry < p.n_pages ? entry : -1;
+    };
+    // Starts the loads of the tile at p0 into buffer `buf`; positions without
+    // a page read page 0.
+    auto load_tile = [&](int p0, int page, int buf) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
+        const int row = (j * kWaves + wave) * kHave;  // the wave's first
+        lds_u16* const to = (lds_u16*)(tiles + buf * 2 * kTileElems + row * D);
         if (kEven) {
-          const int row = j * kPer + wave * (kWave / kLanes);
           const int64_t from =
               (int64_t)max(__builtin_amdgcn_readlane(page, row), 0) * p.page_stride +
               (int64_t)((p0 + row) & page_mask) * width;
-          kn[j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(kh + from) + my_at);
-          vn[j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(vh + from) + my_at);
+          load_lds16(make_rsrc(kh + from, kHave * width * 2), to, my_at, 0);
+          load_lds16(make_rsrc(vh + from, kHave * width * 2), to + kTileElems, my_at, 0);
         } else {
-          const int row = j * kPer + my_row, pg = __shfl(page, row);
+          const int mine = row + lane / kLanes, pg = __shfl(page, mine);
           const int64_t from = (pg < 0 ? 0 : pg * p.page_stride +
-                                (int64_t)((p0 + row) & page_mask) * width) + my_chunk * 8;
-          kn[j] = *reinterpret_cast<const u32x4*>(kh + from);
-          vn[j] = *reinterpret_cast<const u32x4*>(vh + from);
+                                (int64_t)((p0 + mine) & page_mask) * width) + my_chunk * 8;
+          load_lds(kh + from, to);
+          load_lds(vh + from, to + kTileElems);
         }
       }
     };
-    // The loaded tile into buffer `buf`; rows of V that are not there are 0,
-    // infinities and NaN past L are left out and noted.
-    auto store_tile = [&](int p0, int page, int buf, int turn) {
-      uint16_t* const kt = tiles + buf * 2 * kTileElems + my_chunk * 8;
-      if (!(p0 + kUnit <= x.r.L && __all(page >= 0))) {
-        const unsigned long long there = __ballot(page >= 0);
-        const int first = here(my_row);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const int row = j * kPer + first;
-          const bool gone = !(there >> row & 1), own = p0 + row >= x.r.L;
-          uint32_t bad = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t was = vn[j][i], odd = own ? odd_part<T>(was, true) : 0u;
-            vn[j][i] = gone ? 0u : was ^ odd;
-            bad |= odd;
-          }
-          if (bad && !gone) atomicOr(&odd_rows[turn][row / 32], 1u << (row % 32));
-        }
-      }
-#pragma unroll
+    // Waits for the wave's own loads of the tile at p0 and mends its rows of V:
+    // those that are not there become 0, infinities and NaN past L too, noted.
+    auto finish_tile = [&](int p0, int page, int buf, int turn) {
+      TG_WAIT_VM(0);
+      asm volatile("" ::: "memory");
+      if (p0 + kUnit <= x.r.L && __all(page >= 0)) return;
+      const unsigned long long there = __ballot(page >= 0);
+#pragma unroll 1
       for (int j = 0; j < kLoads; ++j) {
-        uint16_t* const to = kt + (j * kPer + my_row) * R::kPitch;
-        *reinterpret_cast<u32x4*>(to) = kn[j];
-        *reinterpret_cast<u32x4*>(to + kTileElems) = vn[j];
+        const int row = (j * kWaves + wave) * kHave + lane / kLanes;
+        const bool gone = !(there >> row & 1), own = p0 + row >= x.r.L;
+        u32x4* const place = reinterpret_cast<u32x4*>(
+            tiles + (buf * 2 + 1) * kTileElems + (j * kWaves + wave) * kHave * D + lane * 8);
+        u32x4 y = *place;
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t odd = own ? odd_part<T>(y[i], true) : 0u;
+          y[i] = gone ? 0u : y[i] ^ odd;
+          bad |= odd;
+        }
+        if (bad && !gone) atomicOr(&odd_rows[turn][row / 32], 1u << (row % 32));
+        *place = y;
       }
     };
 
     int p0 = x.u0 * kUnit, buf = 0, turn = 0;
     const int p_end = x.u1 * kUnit;
-    int page = page_at(p0), page_next = page_at(p0 + kUnit);
-    load_tile(p0, page);
+    int page = page_of(entry_at(p0), p0), entry = entry_at(p0 + kUnit);
     __syncthreads();  // the last piece's reads are over
     if (threadIdx.x < 6) odd_rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
+    load_tile(p0, page, 0);
     __syncthreads();
-    store_tile(p0, page, 0, 0);
+    finish_tile(p0, page, 0, 0);
     __syncthreads();
     for (; p0 < p_end; p0 += kUnit, buf ^= 1) {
       const bool more = p0 + kUnit < p_end;
       const int page_now = page;
+      const uint16_t* const kt = tiles + buf * 2 * kTileElems;
+      f32x4 s[kQ][4];
       if (more) {
-        page = page_next;
-        load_tile(p0 + kUnit, page);
-        page_next = page_at(p0 + 2 * kUnit);
+        page = page_of(entry, p0 + kUnit);
+        load_tile(p0 + kUnit, page, buf ^ 1);
+        entry = entry_at(p0 + 2 * kUnit);
       }
+      if (busy) rows.scores(kt + col * D, k_chunk, s, kh);
       const bool inner = p0 + kUnit <= x.r.L && __all(page_now >= 0);
       if (busy) {
         const unsigned long long there64 = inner ? ~0ull : __ballot(page_now >= 0);
-        const uint16_t* const kt = tiles + buf * 2 * kTileElems;
-        f32x4 s[kQ][4];
-#pragma unroll
-        for (int st = 0; st < R::kSteps; ++st)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const uint4 kf = *reinterpret_cast<const uint4*>(kt + (t * 16 + col) * R::kPitch +
-                                                             st * 32 + quad * 8);
-#pragma unroll
-            for (int c = 0; c < kQ; ++c)
-              s[c][t] = mfma<T>(kf, rows.q[c][st], st ? s[c][t] : f32x4{0, 0, 0, 0});
-          }
         uint32_t see[2][kQ];
         if (!inner) {
 #pragma unroll
@@ -805,8 +839,12 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
         }
         uint4 pr[2][kQ];
         rows.weigh(s, p.c, pr);
-        rows.add(kt + kTileElems, pr[0]);
-        rows.add(kt + kTileElems + kTile * R::kPitch, pr[1]);
+        const uint16_t* const vr = kt + kTileElems + v_row * D + (col & 1) * 4;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          rows.add([&](int h, int d) {
+            return vr + (half * kTile + h * 16) * D + (v_chunk ^ (d * 2)) * 8;
+          }, pr[half], vh);
         if (!inner) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -826,7 +864,7 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
       // one after it (read before the last barrier) cleared.
       const int next = turn == 2 ? 0 : turn + 1;
       if (threadIdx.x < 2) odd_rows[next == 2 ? 0 : next + 1][threadIdx.x] = 0;
-      if (more) store_tile(p0 + kUnit, page, buf ^ 1, next);
+      if (more) finish_tile(p0 + kUnit, page, buf ^ 1, next);
       turn = next;
       __syncthreads();
     }
@@ -1011,7 +1049,6 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
   constexpr int kOcc = occupancy(D, kQ, kShared);
   constexpr int kRows = rows_of(Shape{kQ, kShared});
   constexpr int kUnit = kShared ? 2 * kTile : kWaves * kTile;
-  constexpr int kPitch = Rows<T, D, kQ>::kPitch;
   const tg_kv_cache& c = a->cache;
   const Layout L = layout(a);
   char* w = static_cast<char*>(ws);
@@ -1050,11 +1087,10 @@ hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
   const size_t pre = (size_t)(c.B + 1) * 4;
   hipError_t e;
   if constexpr (kShared) {
-    const size_t lds = (size_t)4 * kUnit * kPitch * 2 + pre;
-    e = c.page_size >= 512 / D ? go(shared_kernel<T, D, kQ, true, kOcc>, lds)
-                               : go(shared_kernel<T, D, kQ, false, kOcc>, lds);
+    e = c.page_size >= 512 / D ? go(shared_kernel<T, D, kQ, true, kOcc>, pre)
+                               : go(shared_kernel<T, D, kQ, false, kOcc>, pre);
   } else {
-    const size_t lds = (size_t)kWaves * kTile * kPitch * 2 + kWaves * kRows * 8 + pre;
+    const size_t lds = (size_t)kWaves * kTile * Rows<T, D, kQ>::kPitch * 2 + kWaves * kRows * 8 + pre;
     e = c.page_size >= kTile   ? go(split_kernel<T, D, kQ, 1, kOcc>, lds)
         : c.page_size == kTile / 2 ? go(split_kernel<T, D, kQ, 2, kOcc>, lds)
                                    : go(split_kernel<T, D, kQ, 0, kOcc>, lds);
