@@ -39,19 +39,31 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
   return v + before;
 }
 
+// A thread's pages of the first round of deal_free(), loaded ahead of the sums
+// that say how many are needed.
+constexpr int kPer = 8;
+struct FirstRefs {
+  int r[kPer];
+  __device__ __forceinline__ FirstRefs(const int32_t* refs, int n_pages) {
+    const int p0 = threadIdx.x * kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) r[i] = p0 + i < n_pages ? refs[p0 + i] : 1;
+  }
+};
+
 // Calls take(k, page) for the k-th free page, k < want, in ascending order of
 // the page; returns how many there were (at most want). Uniform over the block.
 template <class Take>
-__device__ __forceinline__ int deal_free(const int32_t* refs, int n_pages, int want, int* lds,
-                                         Take take) {
-  constexpr int kPer = 8;
+__device__ __forceinline__ int deal_free(const FirstRefs& ahead, const int32_t* refs, int n_pages,
+                                         int want, int* lds, Take take) {
   int found = 0;
   for (int base = 0; base < n_pages && found < want; base += kBlock * kPer) {
     const int p0 = base + threadIdx.x * kPer;
     unsigned free = 0;
     int r[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) r[i] = p0 + i < n_pages ? refs[p0 + i] : 1;
+    for (int i = 0; i < kPer; ++i)
+      r[i] = base == 0 ? ahead.r[i] : p0 + i < n_pages ? refs[p0 + i] : 1;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) free |= (unsigned)(r[i] == 0) << i;
     int total;
@@ -85,6 +97,8 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   __shared__ int lds[kWaves + 1];
   __shared__ int end[kMaxB];        // pages needed up to and with request b
   __shared__ int first[kMaxB + 1];  // q_offsets
+  __shared__ int len[kMaxB];        // lengths; -1: the request gets none
+  const FirstRefs ahead(refs, n_pages);
   const int page = 1 << page_shift;
   int want = 0;
   for (int b0 = 0; b0 < B; b0 += kBlock) {
@@ -93,9 +107,10 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
     if (b < B) {
       first[b] = off[b];
       const int n = max(0, off[b + 1] - off[b]);
-      const long tokens = (long)max(0, lengths[b]) + n;
-      const long pages = (tokens + page - 1) >> page_shift;
+      const int L = max(0, lengths[b]);
+      const long pages = ((long)L + n + page - 1) >> page_shift;
       const int has = max(0, min(held[b], max_pages));
+      len[b] = pages <= max_pages ? L : -1;
       if (pages <= max_pages) need = max(0, (int)pages - has);
     }
     int total;
@@ -105,7 +120,7 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   }
   if (threadIdx.x == 0) first[B] = off[B];
   __syncthreads();
-  const int got = deal_free(refs, n_pages, want, lds, [&](int k, int p) {
+  const int got = deal_free(ahead, refs, n_pages, want, lds, [&](int k, int p) {
     const int b = owner_of(end, B, k), k0 = b ? end[b - 1] : 0;
     refs[p] = 1;
     table[(long)b * max_pages + max(0, held[b]) + (k - k0)] = p;
@@ -113,11 +128,10 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   __syncthreads();
   for (int b = threadIdx.x; b < B; b += kBlock) {
     const int k0 = b ? end[b - 1] : 0, need = end[b] - k0;
-    const int has = max(0, min(held[b], max_pages));
-    const long tokens = (long)max(0, lengths[b]) + max(0, first[b + 1] - first[b]);
-    const bool room = ((tokens + page - 1) >> page_shift) <= max_pages;
-    const bool fits = room && (need == 0 || end[b] <= got);
+    const bool fits = len[b] >= 0 && (need == 0 || end[b] <= got);
+    const int has = need ? max(0, min(held[b], max_pages)) : 0;
     if (!fits) {  // pages dealt to it go back
+      len[b] = -1;
       for (int k = k0; k < min(end[b], got); ++k) {
         int32_t* e = &table[(long)b * max_pages + has + (k - k0)];
         refs[*e] = 0;
@@ -132,8 +146,8 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   for (int r = threadIdx.x; r < T; r += kBlock) {
     const int b = owner_of(first + 1, B, r);
     int slot = -1;
-    if (b < B && r >= first[b] && status[b]) {
-      const int pos = max(0, lengths[b]) + r - first[b];
+    if (b < B && r >= first[b] && len[b] >= 0) {
+      const int pos = len[b] + r - first[b];
       const int p = table[(long)b * max_pages + (pos >> page_shift)];
       if (p >= 0 && p < n_pages) slot = (p << page_shift) | (pos & (page - 1));
     }
@@ -146,8 +160,8 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(
     int32_t* lengths, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int n,
     int32_t* __restrict__ status) {
   __shared__ int lds[kWaves + 1];
-  __shared__ int to[TG_MAX_FORKS], from[TG_MAX_FORKS], len[TG_MAX_FORKS], fresh[TG_MAX_FORKS],
-      end[TG_MAX_FORKS];
+  __shared__ int to[TG_MAX_FORKS], from[TG_MAX_FORKS], len[TG_MAX_FORKS], fresh[TG_MAX_FORKS];
+  const FirstRefs ahead(refs, n_pages);
   const int i = threadIdx.x, page = 1 << page_shift;
   if (i < n) {
     to[i] = dst[i];
@@ -159,22 +173,18 @@ __global__ __launch_bounds__(kBlock) void fork_kernel(
   if (i < n) {
     const int s = from[i], d = to[i];
     good = s >= 0 && s < B && d >= 0 && d < B;
+    const int L = good ? max(0, lengths[s]) : 0;
+    const int of_src = good ? held[s] : 0, of_dst = good ? held[d] : 1;
     for (int j = 0; j < n && good; ++j) good = to[j] != s && (j >= i || to[j] != d);
-    int L = 0;
-    if (good) {
-      L = max(0, lengths[s]);
-      const int pages = (int)(((long)L + page - 1) >> page_shift);
-      good = held[d] == 0 && held[s] >= pages && pages <= max_pages;
-      need = good && (L & (page - 1));
-    }
+    const int pages = (int)(((long)L + page - 1) >> page_shift);
+    good = good && of_dst == 0 && of_src >= pages && pages <= max_pages;
+    need = good && (L & (page - 1));
     len[i] = L;
   }
   int want;
   const int sum = block_scan(need, lds, &want);
-  if (i < n) end[i] = sum;
-  __syncthreads();
   const int got =
-      deal_free(refs, n_pages, want, lds, [&](int k, int p) { fresh[k] = p; });
+      deal_free(ahead, refs, n_pages, want, lds, [&](int k, int p) { fresh[k] = p; });
   __syncthreads();
   const bool fits = good && (need == 0 || sum <= got);
   if (i < n) {

@@ -817,12 +817,12 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
       const int page_now = page;
       const uint16_t* const kt = tiles + buf * 2 * kTileElems;
       f32x4 s[kQ][4];
+      if (busy) rows.scores(kt + col * D, k_chunk, s, kh);
       if (more) {
         page = page_of(entry, p0 + kUnit);
         load_tile(p0 + kUnit, page, buf ^ 1);
         entry = entry_at(p0 + 2 * kUnit);
       }
-      if (busy) rows.scores(kt + col * D, k_chunk, s, kh);
       const bool inner = p0 + kUnit <= x.r.L && __all(page_now >= 0);
       if (busy) {
         const unsigned long long there64 = inner ? ~0ull : __ballot(page_now >= 0);
