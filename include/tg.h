@@ -459,7 +459,7 @@ tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
  * written); positions beyond the page table are not there. The work is dealt
  * evenly over the device whatever the lengths; a request's last bits may
  * depend on the others of its batch, but not on the run. Limit:
- * B * Hkv * (max_nodes * G / 16 + 1) * (max_pages * page_size / 64) < 2^31.
+ * B * Hkv * (max_nodes * G / 16 + 1) * (max_pages * page_size / 64) < 2^30.
  */
 typedef struct {
   tg_kv_cache cache;

@@ -122,9 +122,9 @@ tg_status check_attn(const tg_tree_attn_args* a) {
   // Units of work (64 positions of 16 rows at least) are counted in 32 bits.
   const long long items = (long long)c->B * c->Hkv * (a->max_nodes * (a->Hq / c->Hkv) / 16 + 1);
   const long long units = ((long long)c->max_pages * c->page_size + 63) / 64;
-  if (items > (1LL << 31) / units - 1)
+  if (items > (1LL << 30) / units - 1)
     return set_error(TG_ERR_UNSUPPORTED,
-                     "B * Hkv * (rows per KV head) / 16 * (positions per request) / 64 >= 2^31");
+                     "B * Hkv * (rows per KV head) / 16 * (positions per request) / 64 >= 2^30");
   if (!(a->scale > 0.0f) || a->scale > 1e30f)
     return set_error(TG_ERR_BAD_DIM, "scale must be positive and finite");
   if ((a->T > 0 && (!a->q || !a->out)) || !a->q_offsets || (c->B > 0 && !a->lengths))

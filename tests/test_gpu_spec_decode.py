@@ -176,6 +176,18 @@ ATTN = [
     ([(90, 31)], 8, 1, 256, torch.float16, 128, "chain", True),
     ([(1500, 1)], 40, 1, 128, torch.bfloat16, 16, "tree", False),
     ([(700, 3)] * 9, 4, 4, 64, torch.bfloat16, 2, "tree", False),
+    # Tiles shared by the waves, with an address per lane (tiny pages), and 33
+    # to 64 rows of a KV head.
+    ([(90, 31), (64, 1)], 8, 2, 128, torch.bfloat16, 2, "tree", True),
+    ([(70, 12)], 8, 1, 256, torch.float16, 1, "tree", False),
+    ([(129, 9), (0, 7)], 12, 2, 128, torch.bfloat16, 4, "chain", False),
+    ([(65, 40)], 2, 1, 64, torch.bfloat16, 4, "tree", False),
+    # More requests than a wave has lanes, some without rows.
+    ([(i % 37, i % 3) for i in range(150)], 4, 2, 64, torch.bfloat16, 8, "tree", False),
+    ([(i % 61, 1 + i % 9) for i in range(70)], 8, 1, 128, torch.float16, 16, "tree", False),
+    # One context over many blocks.
+    ([(9000, 2)], 4, 1, 128, torch.bfloat16, 16, "tree", False),
+    ([(5000, 20)], 6, 1, 64, torch.bfloat16, 64, "tree", False),
 ]
 
 
@@ -212,7 +224,8 @@ def test_tree_attention(requests, Hq, Hkv, D, dtype, page, mask, together):
     assert torch.equal(again.view(torch.int16), got.view(torch.int16)), "two runs differ"
 
 
-@pytest.mark.parametrize("Hq,D", [(2, 64), (8, 128), (40, 128), (2, 256)])
+@pytest.mark.parametrize("Hq,D", [(2, 64), (8, 128), (40, 128), (2, 256), (16, 128), (40, 64),
+                                  (16, 256)])
 def test_rows_that_see_nothing_and_masked_nan(Hq, D):
     """Rows without a set bit and without context give zeros; nodes that a row
     does not see hold NaN and infinities and stay out of it."""

@@ -119,6 +119,7 @@ def test_qk_norm_rope_refuses(lib, bad, status):
     (dict(max_nodes=0), tg.TG_ERR_BAD_DIM), (dict(max_nodes=65), tg.TG_ERR_BAD_DIM),
     (dict(max_nodes=2000, mask_words=40), tg.TG_ERR_UNSUPPORTED),
     (dict(mask_words=0), tg.TG_ERR_BAD_DIM), (dict(tree_mask=P + 4), tg.TG_ERR_UNSUPPORTED),
+    (dict(c=cache(B=4096, max_pages=1 << 20)), tg.TG_ERR_UNSUPPORTED),
     (dict(scale=0.0), tg.TG_ERR_BAD_DIM), (dict(scale=float("nan")), tg.TG_ERR_BAD_DIM),
     (dict(scale=float("inf")), tg.TG_ERR_BAD_DIM), (dict(q_stride=504), tg.TG_ERR_BAD_DIM),
     (dict(out_stride=516), tg.TG_ERR_UNSUPPORTED), (dict(q=None), tg.TG_ERR_NULL_ARG),
