@@ -13,9 +13,17 @@
 // positions at a time by itself, K straight from the cache into the operand's
 // layout, V through the wave's own piece of LDS; no wave waits for another
 // until the rows are finished, where the four waves of a block join their
-// maxima, sums and outputs.
-// Many rows (shared kernel): the products bound it. The four waves of a block
-// take different rows and share each tile of 64 positions through LDS.
+// maxima, sums and outputs. 128 single tokens over contexts of up to 8192
+// (heads 32 / 8 of 128): 436 us, 5.6 TB/s; two waves per SIMD without spilled
+// registers are faster than three with (640 us). 7 rows over 131071 positions:
+// 113 us, 4.8 TB/s (blocks get 16 or 17 units: 6 % of them idle at the end).
+// Many rows (shared kernel): the products and the vector unit bound it. The
+// four waves of a block take different rows and share each tile of 64
+// positions through LDS, which the split kernel would read per wave. Eight
+// trees of up to 64 rows over up to 16384 positions (heads 64 / 8 of 128):
+// 185 us, 600 TFLOP/s; the matrix unit works in 35 % of the time, the vector
+// unit (exp, maxima, conversions) in 44 %, LDS in 18 % without bank conflicts,
+// and a wave, of which two fit a SIMD, waits in 42 %.
 //
 // The work is dealt evenly whatever the lengths: all (request, KV head, row
 // tile) items are laid end to end in units of positions, and every block takes
@@ -900,7 +908,8 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
   }
 }
 
-// Joins the parts of the items that several blocks had. As many blocks join an
+// Joins the parts of the items that several blocks had (3 to 14 us; with a
+// grid of one block per item and pair of rows 17 to 45). As many blocks join an
 // item as had a part of it, each an equal share of its rows, so that every
 // block reads about as much as it left. A wave takes 256 / D rows at a time:
 // the waves take different rows, kPass at once, or, where a block has few (one
@@ -1006,7 +1015,13 @@ __global__ __launch_bounds__(kBlock) void join_kernel(const Params p) {
   }
 }
 
-// Which kernel: rows of one KV head at most, over 16-row groups.
+// Which kernel: rows of one KV head at most, over 16-row groups. Up to 32 rows
+// the split kernel reads the cache once per item; above, tiles of 64 rows in a
+// wave by itself take too many registers (64-row trees: 822 us split, 384
+// shared, in the kernels' first forms), and 128 rows per tile halve what is
+// read again for the next 128 (64-row trees 224 us, with 64-row tiles 314).
+// Heads of 256 leave registers for 16 rows a wave (with 32 they spill: a
+// decode batch 223 us instead of 122).
 struct Shape {
   int q;        // 16-row groups per wave
   bool shared;  // waves share tiles (rows over four waves), or split them
