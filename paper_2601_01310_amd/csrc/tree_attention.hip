@@ -1020,8 +1020,7 @@ __global__ __launch_bounds__(kBlock) void join_kernel(const Params p) {
 // wave by itself take too many registers (64-row trees: 822 us split, 384
 // shared, in the kernels' first forms), and 128 rows per tile halve what is
 // read again for the next 128 (64-row trees 224 us, with 64-row tiles 314).
-// Heads of 256 leave registers for 16 rows a wave (with 32 they spill: a
-// decode batch 223 us instead of 122).
+// Heads of 256 leave registers for 16 rows a wave.
 struct Shape {
   int q;        // 16-row groups per wave
   bool shared;  // waves share tiles (rows over four waves), or split them
@@ -1036,8 +1035,9 @@ Shape shape_of(const tg_tree_attn_args* a) {
   return {2, true};
 }
 
-// Waves per SIMD that the registers leave.
-constexpr int occupancy(int D, int q, bool shared) {
+// Waves per SIMD that the registers leave without spills (heads of 256 with
+// two: a decode batch of 64 takes 223 us instead of 122).
+constexpr int occupancy(int D, int q) {
   return D == 64 ? (q == 2 ? 2 : 3) : D == 128 ? 2 : 1;
 }
 
@@ -1050,7 +1050,7 @@ struct Layout {
 Layout layout(const tg_tree_attn_args* a) {
   const Shape sh = shape_of(a);
   const int D = a->cache.D;
-  const size_t blocks = (size_t)kCus * occupancy(D, sh.q, sh.shared);
+  const size_t blocks = (size_t)kCus * occupancy(D, sh.q);
   const size_t slots = 2 * blocks * rows_of(sh);
   Layout L;
   L.part_ml = (2 * blocks * sizeof(Split) + 255) & ~(size_t)255;
@@ -1061,7 +1061,7 @@ Layout layout(const tg_tree_attn_args* a) {
 
 template <class T, int D, int kQ, bool kShared>
 hipError_t launch(const tg_tree_attn_args* a, void* ws, hipStream_t s) {
-  constexpr int kOcc = occupancy(D, kQ, kShared);
+  constexpr int kOcc = occupancy(D, kQ);
   constexpr int kRows = rows_of(Shape{kQ, kShared});
   constexpr int kUnit = kShared ? 2 * kTile : kWaves * kTile;
   const tg_kv_cache& c = a->cache;
