@@ -396,8 +396,8 @@ tg_status tg_kv_restore(const void* store, size_t store_bytes, const uint64_t* c
  * positions are neither read nor written.
  *
  * Limits: page_size a power of two up to 1024, D 64, 128 or 256,
- * n_pages * page_size < 2^31, max_pages * page_size <= 2^30, B <= 4096,
- * Hkv <= 1024, k, v 16-byte aligned, strides
+ * n_pages * page_size < 2^31, max_pages * page_size <= 2^30,
+ * B * max_pages < 2^31, B <= 4096, Hkv <= 1024, k, v 16-byte aligned, strides
  * multiples of 8 elements, page_stride >= page_size * Hkv * D.
  */
 typedef struct {
@@ -496,7 +496,8 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
  * Drawn: the lowest token whose cumulative mass exceeds u_next[b] * the whole
  * mass, in token order; if no mass is left, from p there as it is, and if
  * that has none, token 0. Tokens outside [0, V) are not kept; of two children
- * with one token the second is not. Rows sum to at most about 1 (8 at most).
+ * with one token the second is not. Rows sum to about 1 (beyond 2^17 the sums
+ * are no longer exact and some token of the row comes out).
  * At most max_path nodes are kept, the root among them: deeper ones are
  * ignored. Outputs, for request b: n_out[b] = kept nodes (0 if it has no
  * rows), path [B, max_path] their numbers in order (0 first, then -1),

@@ -35,6 +35,8 @@ tg_status check_cache(const tg_kv_cache* c, bool tables) {
   if ((long long)c->max_pages * c->page_size > (1LL << 30))
     return set_error(TG_ERR_UNSUPPORTED, "max_pages * page_size exceeds 2^30");
   if (c->B > 4096) return set_error(TG_ERR_UNSUPPORTED, "B=%d exceeds 4096", c->B);
+  if ((long long)c->B * c->max_pages >= (1LL << 31))  // pages are counted in 32 bits
+    return set_error(TG_ERR_UNSUPPORTED, "B * max_pages >= 2^31");
   if (c->Hkv > 1024) return set_error(TG_ERR_UNSUPPORTED, "Hkv=%d exceeds 1024", c->Hkv);
   if (c->n_layers > 16384)  // layers of K and of V are a grid dimension
     return set_error(TG_ERR_UNSUPPORTED, "n_layers=%d exceeds 16384", c->n_layers);

@@ -296,15 +296,26 @@ __global__ __launch_bounds__(kBlock) void walk_kernel(const tg_verify_args a, in
   }
 }
 
+// What the threads of a draw tell each other.
+struct Found {
+  double lds[kWaves], at;
+  int bin, token;
+};
+
 // mass(bin) must be the bins' masses of w. Returns the lowest token whose
-// cumulative mass exceeds that drawn by u, -1 if there is no mass.
+// cumulative mass exceeds that drawn by u, -1 if there is no mass. (Rows that
+// sum to more than 2^17 are not added exactly: some token of theirs.)
 template <class Mass>
-__device__ int draw(const Weights& w, int bins, uint64_t u, Mass mass, double* lds, double* at,
-                    int* found) {
+__device__ int draw(const Weights& w, int bins, uint64_t u, Mass mass, Found* f) {
   const int each = (bins + kBlock - 1) / kBlock, b0 = threadIdx.x * each;
   double sum = 0.0, whole;
   for (int i = b0; i < min(bins, b0 + each); ++i) sum += mass(i);
-  const double upto = block_scan(sum, lds, &whole);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    f->bin = bins - 1;
+    f->at = 0.0;
+  }
+  const double upto = block_scan(sum, f->lds, &whole);
   if (whole <= 0.0) return -1;
   const double to = drawn_mass(u, whole);
   if (upto > to && upto - sum <= to) {  // one thread's run of bins
@@ -315,12 +326,13 @@ __device__ int draw(const Weights& w, int bins, uint64_t u, Mass mass, double* l
       if (run + m > to) break;
       run += m;
     }
-    *found = i;
-    *at = to - run;
+    f->bin = i;
+    f->at = to - run;
   }
   __syncthreads();
-  const int lo = *found * kBin + threadIdx.x * 4;
-  const double rest = *at;
+  const int lo = f->bin * kBin + threadIdx.x * 4;
+  const double rest = f->at;
+  if (threadIdx.x == 0) f->token = min(w.V, lo + kBin) - 1;
   double v[4], total;
   weights4(w, lo, wide_rows(w), v);
   for (int j = 0; j < w.n_drop; ++j) {
@@ -330,19 +342,18 @@ __device__ int draw(const Weights& w, int bins, uint64_t u, Mass mass, double* l
       if (t == i) v[i] = 0.0;
   }
   const double mine = (v[0] + v[1]) + (v[2] + v[3]);
-  double run = block_scan(mine, lds, &total) - mine;  // its barriers: *found is read by all
+  double run = block_scan(mine, f->lds, &total) - mine;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (run <= rest && run + v[i] > rest) *found = lo + i;
+    if (run <= rest && run + v[i] > rest) f->token = lo + i;
     run += v[i];
   }
   __syncthreads();
-  return *found;
+  return f->token;
 }
 
 __global__ __launch_bounds__(kBlock) void draw_kernel(const tg_verify_args a, int bins, Space sp) {
-  __shared__ double lds[kWaves], at;
-  __shared__ int found;
+  __shared__ Found found;
   const int b = blockIdx.x;
   const Drawn d = sp.drawn[b];
   if (d.kept == 0) return;
@@ -355,7 +366,7 @@ __global__ __launch_bounds__(kBlock) void draw_kernel(const tg_verify_args a, in
   w.V = a.V;
   const uint64_t u = units24(a.u_next[b]);
   double* const mass = sp.mass + (int64_t)b * bins;
-  int token = draw(w, bins, u, [&](int i) { return mass[i]; }, lds, &at, &found);
+  int token = draw(w, bins, u, [&](int i) { return mass[i]; }, &found);
   if (token < 0) {  // nothing is left: p as it is
     w.q = nullptr;
     w.n_drop = 0;
@@ -365,7 +376,7 @@ __global__ __launch_bounds__(kBlock) void draw_kernel(const tg_verify_args a, in
       if (__lane_id() == 0) mass[bin] = m;
     }
     __syncthreads();
-    token = max(0, draw(w, bins, u, [&](int i) { return mass[i]; }, lds, &at, &found));
+    token = max(0, draw(w, bins, u, [&](int i) { return mass[i]; }, &found));
   }
   if (threadIdx.x == 0) a.tokens_out[(int64_t)b * a.max_path + d.kept - 1] = token;
 }

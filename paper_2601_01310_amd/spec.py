@@ -4,7 +4,9 @@ library's HIP kernels (``include/tg.h`` says what each computes).
 
 Objects bind their tensors once, as :class:`tg.EwForward` does, so that a
 decode loop's calls allocate nothing: new values go into the bound tensors in
-place. ::
+place. A call runs on ``stream``, or on the current stream of the tensors'
+device; who passes another stream than the tensors' own orders it behind what
+filled them and keeps them until it is done. ::
 
     cache = KvCache.empty(n_layers=32, n_pages=4096, page_size=16, Hkv=8, D=128,
                           B=64, max_pages=64, device="cuda")

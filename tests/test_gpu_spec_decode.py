@@ -407,6 +407,90 @@ def _verify(p, tokens, u, un, q=None, mask=None):
     return path[0][:n[0]], t[0][:n[0]]
 
 
+@pytest.mark.parametrize("V", [1000, 160000, 300001])
+def test_rows_that_are_no_distributions_give_a_token_of_theirs(V):
+    """Rows of ones and infinities: sums far beyond exact float64."""
+    p = torch.ones((6, V), device=DEV)
+    p[2:4] = float("inf")
+    p[4:] = 1e30
+    u = torch.tensor([0.0, 0.3, 0.5, 0.7, 0.999, 0.99999997], device=DEV)
+    call = spec.VerifyTree(p, ints([V - 1] * 6), u, u, ints(range(7)), max_path=1)
+    tokens, path, n = (t.cpu().numpy() for t in call())
+    assert (n == 1).all() and (path == 0).all()
+    assert ((tokens >= 0) & (tokens < V)).all()
+    if V == 1000:
+        assert tokens[:, 0].tolist() == (np.floor(u.cpu().double().numpy() * 2 ** 24) * V
+                                         // 2 ** 24).astype(int).tolist()
+
+
+def test_a_whole_step_in_a_graph():
+    """Reserve, norms and rotation, attention (heads of 256), verification,
+    compaction and trim, captured once and replayed on new inputs."""
+    say("a step in a graph")
+    B, n, Hq, Hkv, D, V = 3, 5, 4, 1, 256, 900
+    T = B * n
+    rng = np.random.default_rng(4)
+    cache = spec.KvCache.empty(2, 40, 8, Hkv, D, B, 10, device=DEV)
+    lengths, new, keep = ints([0] * B), ints([0] * B), ints([0] * B)
+    off, slots, status = ints([0, n, 2 * n, T]), ints([0] * T), ints([0] * B)
+    qkv = torch.zeros((T, Hq + 2 * Hkv, D), dtype=torch.bfloat16, device=DEV)
+    mask, tokens = random_masks([n] * B, rng), ints([0] * T)
+    p, u, un = torch.zeros((T, V), device=DEV), torch.zeros(T, device=DEV), torch.zeros(B, device=DEV)
+    rope = spec.QkNormRope(cache, qkv, Hq, None, slots)
+    attend = spec.TreeAttention(cache, rope.q_out, off, lengths, mask)
+    check = spec.VerifyTree(p, tokens, u, un, off, mask, max_path=n)
+
+    def step():
+        cache.reserve(lengths, off, slots, status)
+        for layer in range(2):
+            rope(layer=layer)
+        attend(layer=1)
+        tok, path, kept = check()
+        cache.compact(path, kept, lengths, new)
+        lengths.copy_(new)
+        cache.trim(lengths)
+
+    state = [cache.k, cache.v, cache.page_table, cache.held, cache.refcount, lengths, slots,
+             attend.out, check.tokens_out, check.path, check.n_out]
+
+    def inputs(seed):
+        g = torch.Generator(device=DEV)
+        g.manual_seed(seed)
+        qkv.copy_(torch.randn(qkv.shape, generator=g, device=DEV))
+        p.copy_(torch.softmax(torch.randn(p.shape, generator=g, device=DEV) * 3, 1))
+        tokens.copy_(torch.topk(p, 1).indices[:, 0].roll(1))
+        u.copy_(torch.rand(u.shape, generator=g, device=DEV))
+        un.copy_(torch.rand(un.shape, generator=g, device=DEV))
+
+    def reset():
+        for t in (cache.k, cache.v, cache.held, cache.refcount, lengths):
+            t.zero_()
+        cache.page_table.fill_(-1)
+
+    step()
+    torch.cuda.synchronize()
+    reset()
+    eager = []
+    for seed in range(5):
+        inputs(seed)
+        step()
+        eager.append([t.clone() for t in state])
+    reset()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, capture_error_mode="thread_local"):
+        step()
+    reset()
+    for seed in range(5):
+        inputs(seed)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(state, eager[seed]):
+            assert torch.equal(a, b), seed
+        torch.randn(1000, device=DEV).sum().item()
+    assert int(lengths.min()) >= 5
+
+
 def test_verify_edges():
     nan = float("nan")
     half = [0.5, 0.5, 0.0]

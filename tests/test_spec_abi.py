@@ -41,6 +41,7 @@ CACHE = [
     (dict(n_pages=1 << 27), tg.TG_ERR_UNSUPPORTED),
     (dict(max_pages=1 << 27), tg.TG_ERR_UNSUPPORTED),
     (dict(n_layers=20000), tg.TG_ERR_UNSUPPORTED),
+    (dict(B=4096, max_pages=1 << 19, page_size=1, page_stride=256), tg.TG_ERR_UNSUPPORTED),
     (dict(page_stride=16 * 256 - 8), tg.TG_ERR_BAD_DIM),
     (dict(page_stride=16 * 256 + 4), tg.TG_ERR_UNSUPPORTED),
     (dict(layer_stride=-8), tg.TG_ERR_UNSUPPORTED),
