@@ -31,6 +31,7 @@
 // parts (float32, not normalised, with m and the sum) in the workspace, and a
 // second kernel joins those.
 #include "tg_kv.h"
+#include "tg_tree.h"
 
 namespace tg {
 namespace {
@@ -343,22 +344,8 @@ struct Rows {
   // those that are `there`.
   __device__ __forceinline__ uint32_t sees(const Params& p, const uint64_t* __restrict__ mask,
                                            const Piece& x, int c, int p0, uint32_t there) const {
-    const int j0 = p0 - x.r.L;  // node at the first position
-    if (j0 <= -32) return there;
-    const int ctx = max(0, -j0), n0 = max(0, j0);
-    uint32_t own;
-    if (mask) {
-      const uint64_t* w = mask + (int64_t)(x.r.first + node[c]) * p.words + n0 / 64;
-      const int sh = n0 % 64;
-      uint64_t v = w[0] >> sh;
-      if (sh > 32 && n0 / 64 + 1 < p.words) v |= w[1] << (64 - sh);
-      own = (uint32_t)v;
-    } else {
-      const int k = node[c] - n0 + 1;
-      own = k >= 32 ? ~0u : k > 0 ? (1u << k) - 1 : 0u;
-    }
-    if (x.r.n - n0 < 32) own &= (1u << max(x.r.n - n0, 0)) - 1;
-    return there & (ctx ? own << ctx | ((1u << ctx) - 1) : own);
+    return seen_bits(mask ? mask + (int64_t)(x.r.first + node[c]) * p.words : mask, p.words, node[c],
+                     x.r.n, x.r.L, p0, there);
   }
 
   // Scores of a tile of 64 positions in LDS, rows D apart: `kt` is the lane's
