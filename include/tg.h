@@ -541,6 +541,13 @@ tg_status tg_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
  * gets and takes none (status[b] 0 instead of 1). slots [T] is where each new
  * row goes in the cache (page * page_size + row), -1 where its request got no
  * pages. A request may already hold the pages that it needs.
+ *
+ * No slot lies in a page that another request holds: after a fork, lengths[b]
+ * may have gone back to fewer tokens than are shared, and the shared pages that
+ * new rows would lie in are then replaced by fresh ones (they count as pages
+ * needed, before the new ones), with the tokens in use copied in every layer,
+ * and the request's references to the old ones drop. The reference counts
+ * before the call decide which pages are shared.
  */
 tg_status tg_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
                               const int32_t* q_offsets, int T, int32_t* slots, int32_t* status,

@@ -204,25 +204,37 @@ class Pages:
         B, width = self.table.shape
         slots, status = np.full(T, -1, np.int32), np.zeros(B, np.int32)
         free, short = int((self.ref == 0).sum()), False
+        before, dropped = self.ref.copy(), []
         for b in range(B):
-            n = max(0, int(q_offsets[b + 1] - q_offsets[b]))
-            want = self.pages_of(max(0, int(lengths[b])) + n)
-            need = max(0, want - int(self.held[b]))
+            n, L = max(0, int(q_offsets[b + 1] - q_offsets[b])), max(0, int(lengths[b]))
+            want = self.pages_of(L + n)
             if want > width:
                 continue
-            short = short or need > free
-            if need and short:
+            # Held pages that new rows would lie in and that others hold too.
+            shared = [j for j in range(L // self.size, min(int(self.held[b]), want))
+                      if n and 0 <= self.table[b, j] < len(before) and before[self.table[b, j]] > 1]
+            new = max(0, want - int(self.held[b]))
+            short = short or len(shared) + new > free
+            if shared + [0] * new and short:
                 continue
-            free -= need
-            for _ in range(need):
+            free -= len(shared) + new
+            for j in shared:
+                old, p = int(self.table[b, j]), self._take()
+                used = L % self.size if j == L // self.size else 0
+                for c in self.caches:
+                    c[:, p, :used] = c[:, old, :used]
+                self.table[b, j] = p
+                dropped.append(old)
+            for _ in range(new):
                 self.table[b, self.held[b]] = self._take()
                 self.held[b] += 1
             status[b] = 1
             for i in range(n):
-                pos = max(0, int(lengths[b])) + i
-                p = self.table[b, pos // self.size]
+                p = self.table[b, (L + i) // self.size]
                 if p >= 0:
-                    slots[q_offsets[b] + i] = p * self.size + pos % self.size
+                    slots[q_offsets[b] + i] = p * self.size + (L + i) % self.size
+        for p in dropped:
+            self.ref[p] -= 1
         return slots, status
 
     def fork(self, lengths, src, dst):

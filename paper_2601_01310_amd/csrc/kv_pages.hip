@@ -94,28 +94,63 @@ __device__ __forceinline__ int owner_of(const int* end, int n, int k) {
   return lo;
 }
 
+// Calls f(i, j, page) for the i-th of the pages that hold some of the positions
+// [L, L + n) and that the request (`row` of the table, `held` pages) shares;
+// returns their number. There is a new row in each, so i < n.
+template <class F>
+__device__ __forceinline__ int shared_pages(const int32_t* row, const int32_t* refs, int n_pages,
+                                            int page_shift, int L, int n, int held, F f) {
+  int i = 0;
+  const int end = n > 0 ? min(held, ((L + n - 1) >> page_shift) + 1) : 0;
+  for (int j = L >> page_shift; j < end; ++j) {
+    const int p = row[j];
+    if (p >= 0 && p < n_pages && refs[p] > 1) f(i++, j, p);
+  }
+  return i;
+}
+
+// New rows never land in a page that others hold too (after a fork, a request
+// may go back to fewer tokens than it shares): such a page is replaced by a
+// fresh one with the tokens in use copied. The counts before the call decide,
+// so every request that would write gets a copy of its own, whatever the order.
+// A rollback below a fork is rare: the block that keeps the tables copies too,
+// a wave per layer's K or V.
 __global__ __launch_bounds__(kBlock) void reserve_kernel(
     int32_t* table, int32_t* held, int32_t* refs, int n_pages, int page_shift, int B, int max_pages,
-    const int32_t* __restrict__ lengths, const int32_t* __restrict__ off, int T,
-    int32_t* __restrict__ slots, int32_t* __restrict__ status) {
+    const int32_t* __restrict__ lengths, const int32_t* __restrict__ off, int T, int32_t* slots,
+    int32_t* __restrict__ status, uint16_t* k, uint16_t* v, int64_t layer_stride,
+    int64_t page_stride, int n_layers, int width) {
   __shared__ int lds[kWaves + 1];
   __shared__ int end[kMaxB];        // pages needed up to and with request b
   __shared__ int first[kMaxB + 1];  // q_offsets
   __shared__ int len[kMaxB];        // lengths; -1: the request gets none
+  __shared__ int copies[kMaxB];     // pages of request b to be replaced
+  __shared__ int any_copies;
   const FirstRefs ahead(refs, n_pages);
   const int page = 1 << page_shift;
+  // The shared pages among those of request b's new rows. Until the rows' own
+  // slots are written, slots[first[b] + i] keeps the page that replaces the
+  // i-th, then the page that it replaced.
+  auto shared_of = [&](int b, int n, int L, int has, auto f) {
+    return shared_pages(table + (long)b * max_pages, refs, n_pages, page_shift, L, n, has, f);
+  };
+  if (threadIdx.x == 0) any_copies = 0;
   int want = 0;
   for (int b0 = 0; b0 < B; b0 += kBlock) {
     const int b = b0 + threadIdx.x;
     int need = 0;
     if (b < B) {
-      first[b] = off[b];
-      const int n = max(0, off[b + 1] - off[b]);
+      const int at = off[b], n = max(0, off[b + 1] - at);
       const int L = max(0, lengths[b]);
       const long pages = ((long)L + n + page - 1) >> page_shift;
       const int has = max(0, min(held[b], max_pages));
+      first[b] = at;
       len[b] = pages <= max_pages ? L : -1;
-      if (pages <= max_pages) need = max(0, (int)pages - has);
+      copies[b] = 0;
+      if (pages <= max_pages) {
+        if (at >= 0 && n <= T - at) copies[b] = shared_of(b, n, L, has, [](int, int, int) {});
+        need = max(0, (int)pages - has) + copies[b];
+      }
     }
     int total;
     const int sum = block_scan(need, lds, &total);
@@ -125,28 +160,67 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   if (threadIdx.x == 0) first[B] = off[B];
   __syncthreads();
   const int got = deal_free(ahead, refs, n_pages, want, lds, [&](int k, int p) {
-    const int b = owner_of(end, B, k), k0 = b ? end[b - 1] : 0;
+    const int b = owner_of(end, B, k), i = k - (b ? end[b - 1] : 0), c = copies[b];
     refs[p] = 1;
-    table[(long)b * max_pages + max(0, held[b]) + (k - k0)] = p;
+    if (i < c) slots[first[b] + i] = p;
+    else table[(long)b * max_pages + max(0, held[b]) + (i - c)] = p;
   });
   __syncthreads();
   for (int b = threadIdx.x; b < B; b += kBlock) {
-    const int k0 = b ? end[b - 1] : 0, need = end[b] - k0;
+    const int k0 = b ? end[b - 1] : 0, need = end[b] - k0, c = copies[b];
     const bool fits = len[b] >= 0 && (need == 0 || end[b] <= got);
-    const int has = need ? max(0, min(held[b], max_pages)) : 0;
+    const int has = need > c ? max(0, min(held[b], max_pages)) : 0;
     if (!fits) {  // pages dealt to it go back
       len[b] = -1;
-      for (int k = k0; k < min(end[b], got); ++k) {
-        int32_t* e = &table[(long)b * max_pages + has + (k - k0)];
+      for (int i = 0; i < min(end[b], got) - k0; ++i) {
+        int32_t* e = i < c ? &slots[first[b] + i] : &table[(long)b * max_pages + has + (i - c)];
         refs[*e] = 0;
         *e = -1;
       }
-    } else if (need) {
-      held[b] = has + need;
+      copies[b] = 0;
+    } else {
+      if (need > c) held[b] = has + need - c;
+      if (c) any_copies = 1;
     }
     status[b] = fits;
   }
   __syncthreads();
+  if (any_copies) {
+    const int lane = threadIdx.x % kWave;
+    for (int b = 0; b < B; ++b) {
+      if (copies[b] == 0) continue;
+      shared_of(b, first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
+        const int rows = j == len[b] >> page_shift ? len[b] & (page - 1) : 0;
+        const int fresh = slots[first[b] + i], chunks = rows * (width / 8);
+        for (int l = threadIdx.x / kWave; l < 2 * n_layers; l += kWaves) {
+          uint16_t* const base = (l & 1 ? v : k) + (int64_t)(l >> 1) * layer_stride;
+          const uint4* s = reinterpret_cast<const uint4*>(base + p * page_stride);
+          uint4* o = reinterpret_cast<uint4*>(base + fresh * page_stride);
+          constexpr int kU = 4;
+          for (int c0 = lane; c0 < chunks; c0 += kWave * kU) {
+            uint4 x[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+              if (c0 + u * kWave < chunks) x[u] = s[c0 + u * kWave];
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+              if (c0 + u * kWave < chunks) o[c0 + u * kWave] = x[u];
+          }
+        }
+      });
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < B; b += kBlock)
+      if (copies[b])
+        shared_of(b, first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
+          table[(long)b * max_pages + j] = slots[first[b] + i];
+          slots[first[b] + i] = p;
+        });
+    __syncthreads();
+    for (int b = threadIdx.x; b < B; b += kBlock)
+      for (int i = 0; i < copies[b]; ++i) atomicSub(&refs[slots[first[b] + i]], 1);
+    __syncthreads();
+  }
   for (int r = threadIdx.x; r < T; r += kBlock) {
     const int b = owner_of(first + 1, B, r);
     int slot = -1;
@@ -338,7 +412,9 @@ hipError_t launch_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
   if (c->B == 0) return hipSuccess;
   hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kBlock), 0, s, c->page_table, c->held,
                      c->refcount, c->n_pages, __builtin_ctz(c->page_size), c->B, c->max_pages,
-                     lengths, q_offsets, T, slots, status);
+                     lengths, q_offsets, T, slots, status, static_cast<uint16_t*>(c->k),
+                     static_cast<uint16_t*>(c->v), c->layer_stride, c->page_stride, c->n_layers,
+                     c->Hkv * c->D);
   return hipGetLastError();
 }
 

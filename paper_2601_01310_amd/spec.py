@@ -134,7 +134,8 @@ class KvCache:
                    torch.zeros(B, **ints), torch.zeros(n_pages, **ints))
 
     def reserve(self, lengths, q_offsets, slots, status, stream=None):
-        """Pages for the new rows; fills ``slots`` [T] and ``status`` [B]."""
+        """Pages for the new rows, none of which others hold; fills ``slots`` [T]
+        and ``status`` [B]."""
         B, d = self.args.B, self._device
         _check(tg.load().tg_kv_pages_reserve(
             self._ref, _int32(lengths, "lengths", d, B), _int32(q_offsets, "q_offsets", d, B + 1),

@@ -29,3 +29,42 @@ def test_trees_that_fill_their_mask_words(n, Hq, Hkv, D, dtype, page):
     mask = random_masks([n] * len(L), rng)
     out = spec.TreeAttention(cache, q, ints(off), ints(L), mask, max_nodes=n)()
     check_attention(out, f64(q), cache, table, 0, off, L, mask, 1 / math.sqrt(D), dtype)
+
+
+@pytest.mark.parametrize("page,together,trim", [(16, False, True), (8, True, False)])
+def test_rows_after_a_rollback_below_a_fork_leave_the_parent_alone(page, together, trim):
+    """A child goes back to fewer tokens than it shares and writes new rows:
+    the parent's rows keep their bits, and so do the child's remaining ones."""
+    say(f"rollback below a fork, page {page}")
+    rng = np.random.default_rng(page)
+    n, back = 2 * page, 2 * page - page // 2 - 1
+    cache, _ = make_pool([n, 0], page, 2, 64, torch.bfloat16, rng, layers=3, together=together,
+                         spare=6)
+    lengths, status = ints([n, 0]), ints([7])
+    cache.fork(lengths, ints([0]), ints([1]), status)
+    assert status.tolist() == [1] and lengths.tolist() == [n, n]
+    lengths.copy_(ints([n, back]))
+    if trim:
+        cache.trim(lengths)
+
+    def tokens(b, m):
+        table = cache.page_table[b].tolist()
+        return torch.stack([x[:, table[p // page], p % page] for x in (cache.k, cache.v)
+                            for p in range(m)])
+
+    parent, child = tokens(0, n), tokens(1, back)
+    rows = page + 3
+    off, slots, status = ints([0, 0, rows]), ints([9] * rows), ints([9, 9])
+    cache.reserve(lengths, off, slots, status)
+    assert status.tolist() == [1, 1]
+    refs = cache.refcount.tolist()
+    assert all(refs[s // page] == 1 for s in slots.tolist())
+    qkv = torch.randn((rows, 8, 64), device=DEV).to(torch.bfloat16)
+    rope = spec.QkNormRope(cache, qkv, 4, None, slots)
+    for layer in range(3):
+        rope(layer=layer)
+    assert torch.equal(tokens(0, n), parent)
+    assert torch.equal(tokens(1, back), child)
+    new = tokens(1, back + rows).view(2, back + rows, 3, 2, 64)[:, back:]
+    assert torch.equal(new[0], qkv[:, None, 4:6].expand(-1, 3, -1, -1))
+    assert torch.equal(new[1], qkv[:, None, 6:].expand(-1, 3, -1, -1))
