@@ -456,10 +456,13 @@ tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
  * product with v. A row that sees nothing gives zeros. Positions that a row
  * does not see do not reach it, whatever they hold (infinities and NaN
  * included). max_nodes bounds the nodes per request (rows beyond it are not
- * written); positions beyond the page table are not there. The work is dealt
- * evenly over the device whatever the lengths; a request's last bits may
- * depend on the others of its batch, but not on the run. Limit:
- * B * Hkv * (max_nodes * G / 16 + 1) * (max_pages * page_size / 64) < 2^30.
+ * written); positions beyond the page table are not there. typical_nodes is how
+ * many rows most requests have, if max_nodes says little about it (0: max_nodes):
+ * the kernel is chosen for it, any choice is right. The work is dealt evenly
+ * over the device whatever the lengths; a request's last bits may depend on the
+ * others of its batch, but not on the run. With G' = G / 16, the limit is
+ *   Hkv * min(B * (max_nodes * G' + 1), T * G' + B) * max_pages * page_size / 64
+ *     < 2^30.
  */
 typedef struct {
   tg_kv_cache cache;
@@ -471,6 +474,7 @@ typedef struct {
   const int32_t* lengths;    /* [B] */
   const uint64_t* tree_mask; /* [T, mask_words], or NULL */
   void* out;
+  int typical_nodes;
 } tg_tree_attn_args;
 
 size_t tg_tree_attention_workspace(const tg_tree_attn_args* a);

@@ -121,12 +121,17 @@ tg_status check_attn(const tg_tree_attn_args* a) {
   if ((st = check_nodes(a->max_nodes, a->tree_mask, a->mask_words)) != TG_OK) return st;
   if ((st = check_stride("q_stride", a->q_stride, (int64_t)a->Hq * c->D)) != TG_OK) return st;
   if ((st = check_stride("out_stride", a->out_stride, (int64_t)a->Hq * c->D)) != TG_OK) return st;
+  if (a->typical_nodes < 0)
+    return set_error(TG_ERR_BAD_DIM, "typical_nodes=%d must be >= 0", a->typical_nodes);
   // Units of work (64 positions of 16 rows at least) are counted in 32 bits.
-  const long long items = (long long)c->B * c->Hkv * (a->max_nodes * (a->Hq / c->Hkv) / 16 + 1);
+  const long long G = a->Hq / c->Hkv;
+  const long long by_request = (long long)c->B * (a->max_nodes * G / 16 + 1);
+  const long long by_row = a->T * G / 16 + c->B;
+  const long long items = c->Hkv * (by_row < by_request ? by_row : by_request);
   const long long units = ((long long)c->max_pages * c->page_size + 63) / 64;
   if (items > (1LL << 30) / units - 1)
     return set_error(TG_ERR_UNSUPPORTED,
-                     "B * Hkv * (rows per KV head) / 16 * (positions per request) / 64 >= 2^30");
+                     "Hkv * (16-row tiles of all requests) * (positions per request) / 64 >= 2^30");
   if (!(a->scale > 0.0f) || a->scale > 1e30f)
     return set_error(TG_ERR_BAD_DIM, "scale must be positive and finite");
   if ((a->T > 0 && (!a->q || !a->out)) || !a->q_offsets || (c->B > 0 && !a->lengths))

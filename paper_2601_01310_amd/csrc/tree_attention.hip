@@ -39,6 +39,7 @@ namespace {
 constexpr int kBlock = 256, kWaves = kBlock / kWave;
 constexpr int kTile = 32;  // positions per pair of products
 constexpr int kCus = 256;
+constexpr int kMostUnits = (1 << 30) - 1;
 constexpr float kLazy = 8.0f;  // how far (in powers of two) a score may pass m
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -114,6 +115,10 @@ __device__ __forceinline__ float sum4(float x) {
   x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
 }
+
+// Sums of units of work. The host's check keeps them below kMostUnits for
+// offsets that ascend; others, whose requests overlap, stay inside all arrays.
+__device__ __forceinline__ int add_units(int a, int b) { return min(a + b, kMostUnits); }
 
 // 2^(a - b) with 0 where a is -infinity.
 __device__ __forceinline__ float grow(float a, float b) {
@@ -207,7 +212,7 @@ struct Dealer {
 #pragma unroll
       for (int m = 1; m < kWave; m *= 2) {
         const int o = __shfl_up(sum, m);
-        if (lane >= m) sum += o;
+        if (lane >= m) sum = add_units(sum, o);
       }
       const int before = sum - units;
       if (wave == 0 && lane < p.B) pre[lane + 1] = sum;
@@ -237,17 +242,17 @@ struct Dealer {
 #pragma unroll
       for (int m = 1; m < kWave; m *= 2) {
         const int o = __shfl_up(x, m);
-        if (lane >= m) x += o;
+        if (lane >= m) x = add_units(x, o);
       }
       __syncthreads();
       if (lane == kWave - 1) carry[wave] = x;
       __syncthreads();
       int front = base;
       for (int i = 0; i < kWaves; ++i) {
-        if (i < wave) front += carry[i];
-        base += carry[i];
+        if (i < wave) front = add_units(front, carry[i]);
+        base = add_units(base, carry[i]);
       }
-      if (b < p.B) pre[b + 1] = front + x;
+      if (b < p.B) pre[b + 1] = add_units(front, x);
     }
     if (threadIdx.x == 0) pre[0] = 0;
     __syncthreads();
@@ -295,7 +300,7 @@ struct Dealer {
     Split s;
     const int start = unit - x.u0;  // the item's first unit
     s.k0 = start / share;
-    s.parts = (start + x.r.units - 1) / share - s.k0 + 1;
+    s.parts = min((start + x.r.units - 1) / share, (int)gridDim.x - 1) - s.k0 + 1;
     s.at = me - s.k0;
     s.slot = start == s.k0 * share ? 0 : 1;
     s.first = x.r.first;
@@ -1002,7 +1007,8 @@ __global__ __launch_bounds__(kBlock) void join_kernel(const Params p) {
   }
 }
 
-// Which kernel: rows of one KV head at most, over 16-row groups. Up to 32 rows
+// Which kernel: the rows of one KV head that requests have (at most, or as a
+// caller who cannot say so expects), over 16-row groups. Up to 32 rows
 // the split kernel reads the cache once per item; above, tiles of 64 rows in a
 // wave by itself take too many registers (64-row trees: 822 us split, 384
 // shared, in the kernels' first forms), and 128 rows per tile halve what is
@@ -1014,7 +1020,9 @@ struct Shape {
 };
 
 Shape shape_of(const tg_tree_attn_args* a) {
-  const int rows = a->max_nodes * (a->Hq / a->cache.Hkv);
+  const int nodes = a->typical_nodes > 0 && a->typical_nodes < a->max_nodes ? a->typical_nodes
+                                                                           : a->max_nodes;
+  const int rows = nodes * (a->Hq / a->cache.Hkv);
   if (rows <= 16) return {1, false};
   if (a->cache.D == 256) return {1, true};
   if (rows <= 32) return {2, false};

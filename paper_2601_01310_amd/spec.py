@@ -220,8 +220,9 @@ def _mask(tree_mask, T) -> int:
 class TreeAttention:
     """Attention of ``q`` [T, Hq, D] over the cache; returns ``out`` (a tensor
     of its own if not given). ``tree_mask`` [T, W] int64 (the bits of tg.h's
-    uint64 words) or None for chains; ``max_nodes`` bounds a request's rows
-    (by default by T)."""
+    uint64 words) or None for chains; ``max_nodes`` bounds a request's rows. By
+    default T does, and the kernel is chosen for the mean, T / B: give it where
+    some requests have many more rows than others."""
 
     def __init__(self, cache: KvCache, q, q_offsets, lengths, tree_mask=None, scale=None,
                  max_nodes=None, out=None):
@@ -237,11 +238,12 @@ class TreeAttention:
         _want(lengths, "lengths", torch.int32, (c.B,))
         words = _mask(tree_mask, T)
         _same_device(cache.k, q, out, q_offsets, lengths, tree_mask)
+        a = self.args = tg.TreeAttnArgs()
         if max_nodes is None:
             max_nodes = max(1, min(T, tg.MAX_NODES, 64 * words if words else tg.MAX_NODES))
+            a.typical_nodes = -(-T // max(1, c.B))
         self._keep = (cache, q, q_offsets, lengths, tree_mask)
         self.out = out
-        a = self.args = tg.TreeAttnArgs()
         a.cache, a.T, a.Hq, a.max_nodes, a.mask_words = c, T, Hq, max_nodes, words
         a.scale = 1.0 / math.sqrt(c.D) if scale is None else scale
         a.q_stride, a.out_stride = stride, out_stride

@@ -82,7 +82,8 @@ class TreeAttnArgs(ctypes.Structure):
     """Mirror of ``tg_tree_attn_args``."""
     _fields_ = [("cache", KvCacheArgs)] + _fields([
         ("int", "layer T Hq max_nodes mask_words"), ("float", "scale"),
-        ("i64", "q_stride out_stride"), ("ptr", "q q_offsets lengths tree_mask out")])
+        ("i64", "q_stride out_stride"), ("ptr", "q q_offsets lengths tree_mask out"),
+        ("int", "typical_nodes")])
 
 
 class VerifyArgs(ctypes.Structure):

@@ -68,3 +68,36 @@ def test_rows_after_a_rollback_below_a_fork_leave_the_parent_alone(page, togethe
     new = tokens(1, back + rows).view(2, back + rows, 3, 2, 64)[:, back:]
     assert torch.equal(new[0], qkv[:, None, 4:6].expand(-1, 3, -1, -1))
     assert torch.equal(new[1], qkv[:, None, 6:].expand(-1, 3, -1, -1))
+
+
+def test_a_decode_batch_takes_the_kernel_of_single_rows_by_default():
+    say("attention, decode batch without max_nodes")
+    rng = np.random.default_rng(11)
+    L = rng.integers(0, 90, 130).tolist()
+    cache, table = make_pool([x + 1 for x in L], 16, 2, 128, torch.bfloat16, rng)
+    q = torch.randn((130, 8, 128), device=DEV).to(torch.bfloat16)
+    off = list(range(131))
+    by_default = spec.TreeAttention(cache, q, ints(off), ints(L))
+    told = spec.TreeAttention(cache, q, ints(off), ints(L), max_nodes=1)
+    assert by_default.ws_bytes == told.ws_bytes
+    assert torch.equal(by_default(), told())
+    check_attention(told.out, f64(q), cache, table, 0, off, L, None, 1 / math.sqrt(128),
+                    torch.bfloat16)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,dtype,page", [
+    (4, 1, 128, torch.bfloat16, 16), (6, 1, 64, torch.float16, 32), (2, 1, 256, torch.bfloat16, 4),
+    (40, 2, 64, torch.bfloat16, 8)])
+def test_a_long_request_among_short_ones_without_max_nodes(Hq, Hkv, D, dtype, page):
+    """Many row tiles of a kernel that is chosen for few rows."""
+    say(f"attention, one request of 90 rows among 40 of one, Hq={Hq} D={D}")
+    rng = np.random.default_rng(D)
+    N = [1] * 20 + [90, 0] + [1] * 20
+    L = rng.integers(0, 200, len(N)).tolist()
+    cache, table = make_pool([a + b for a, b in zip(L, N)], page, Hkv, D, dtype, rng)
+    off = np.concatenate([[0], np.cumsum(N)]).astype(np.int32)
+    q = torch.randn((int(off[-1]), Hq, D), device=DEV).to(dtype)
+    mask = random_masks(N, rng)
+    for m in (mask, None):
+        call = spec.TreeAttention(cache, q, torch.from_numpy(off).to(DEV), ints(L), m)
+        check_attention(call(), f64(q), cache, table, 0, off, L, m, 1 / math.sqrt(D), dtype)
