@@ -4,9 +4,9 @@ library's HIP kernels (``include/tg.h`` says what each computes).
 
 Objects bind their tensors once, as :class:`tg.EwForward` does, so that a
 decode loop's calls allocate nothing: new values go into the bound tensors in
-place. A call runs on ``stream``, or on the current stream of the tensors'
-device; who passes another stream than the tensors' own orders it behind what
-filled them and keeps them until it is done. ::
+place. A call runs on the tensors' device, whichever is current, on ``stream``
+or on that device's current stream; who passes another stream than the tensors'
+own orders it behind what filled them and keeps them until it is done. ::
 
     cache = KvCache.empty(n_layers=32, n_pages=4096, page_size=16, Hkv=8, D=128,
                           B=64, max_pages=64, device="cuda")
@@ -60,16 +60,25 @@ def _rows(t: torch.Tensor, name: str, dtype, inner) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(dense, t.stride(0))
 
 
-def _stream(stream, device: int) -> int:
-    """Raw handle of ``stream``, or of the current one of the tensors' device."""
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _run(call, device: int, stream, *args):
+    """A call of the library with ``args`` and the stream. ``device``, the
+    tensors', is made the current one for it: kernels start there, and a null
+    stream is the current device's."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device)
-    return stream if isinstance(stream, int) else stream.cuda_stream
-
-
-def _check(status: int, where: str):
+        stream = _current_stream(device)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    if _current_device() == device:
+        status = call(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, stream)
     if status != tg.TG_OK:
-        raise tg.TgError(status, where)
+        raise tg.TgError(status, call.__name__)
 
 
 def _int32(t: torch.Tensor, name: str, device: int, n: int, dim: int = 1) -> int:
@@ -121,7 +130,7 @@ class KvCache:
         a.page_stride = k.stride(1) if pages > 1 else size * Hkv * D
         a.k, a.v, a.page_table = k.data_ptr(), v.data_ptr(), page_table.data_ptr()
         a.held, a.refcount = held.data_ptr(), refcount.data_ptr()
-        self._ref, self._device = ctypes.byref(a), k.get_device()
+        self._ref, self._device, self._lib = ctypes.byref(a), k.get_device(), tg.load()
 
     @classmethod
     def empty(cls, n_layers, n_pages, page_size, Hkv, D, B, max_pages, dtype=torch.bfloat16,
@@ -137,33 +146,29 @@ class KvCache:
         """Pages for the new rows, none of which others hold; fills ``slots`` [T]
         and ``status`` [B]."""
         B, d = self.args.B, self._device
-        _check(tg.load().tg_kv_pages_reserve(
-            self._ref, _int32(lengths, "lengths", d, B), _int32(q_offsets, "q_offsets", d, B + 1),
-            slots.shape[0], _int32(slots, "slots", d, -1), _int32(status, "status", d, B),
-            _stream(stream, d)), "tg_kv_pages_reserve")
+        _run(self._lib.tg_kv_pages_reserve, d, stream, self._ref, _int32(lengths, "lengths", d, B),
+             _int32(q_offsets, "q_offsets", d, B + 1), slots.shape[0],
+             _int32(slots, "slots", d, -1), _int32(status, "status", d, B))
 
     def fork(self, lengths, src, dst, status, stream=None):
         """Requests ``dst`` become copies of ``src``; updates ``lengths``."""
         n, d = src.shape[0], self._device
-        _check(tg.load().tg_kv_pages_fork(
-            self._ref, _int32(lengths, "lengths", d, self.args.B), _int32(src, "src", d, n),
-            _int32(dst, "dst", d, n), n, _int32(status, "status", d, n), _stream(stream, d)),
-            "tg_kv_pages_fork")
+        _run(self._lib.tg_kv_pages_fork, d, stream, self._ref,
+             _int32(lengths, "lengths", d, self.args.B), _int32(src, "src", d, n),
+             _int32(dst, "dst", d, n), n, _int32(status, "status", d, n))
 
     def trim(self, keep, stream=None):
         """Gives back the pages past ``keep`` [B] tokens of each request."""
-        _check(tg.load().tg_kv_pages_trim(
-            self._ref, _int32(keep, "keep", self._device, self.args.B),
-            _stream(stream, self._device)), "tg_kv_pages_trim")
+        _run(self._lib.tg_kv_pages_trim, self._device, stream, self._ref,
+             _int32(keep, "keep", self._device, self.args.B))
 
     def compact(self, path, n_keep, lengths, new_lengths, stream=None):
         """Moves the kept rows of every layer together (``path`` [B, max_path]
         and ``n_keep`` [B] as :class:`VerifyTree` returns them)."""
         B, d, most = self.args.B, self._device, path.shape[-1]
-        _check(tg.load().tg_kv_compact(
-            self._ref, _int32(path, "path", d, B * most, 2), most, _int32(n_keep, "n_keep", d, B),
-            _int32(lengths, "lengths", d, B), _int32(new_lengths, "new_lengths", d, B),
-            _stream(stream, d)), "tg_kv_compact")
+        _run(self._lib.tg_kv_compact, d, stream, self._ref, _int32(path, "path", d, B * most, 2),
+             most, _int32(n_keep, "n_keep", d, B), _int32(lengths, "lengths", d, B),
+             _int32(new_lengths, "new_lengths", d, B))
 
 
 class QkNormRope:
@@ -199,13 +204,12 @@ class QkNormRope:
         for name, t in dict(qkv=qkv, q_weight=q_weight, k_weight=k_weight, cos_sin=cos_sin,
                             positions=positions, slots=slots, q_out=q_out).items():
             setattr(a, name, None if t is None else t.data_ptr())
-
         self._ref, self._device = ctypes.byref(a), qkv.get_device()
+        self._call = tg.load().tg_qk_norm_rope
 
     def __call__(self, layer=0, stream=None):
         self.args.layer = layer
-        _check(tg.load().tg_qk_norm_rope(self._ref, _stream(stream, self._device)),
-               "tg_qk_norm_rope")
+        _run(self._call, self._device, stream, self._ref)
         return self.q_out
 
 
@@ -256,11 +260,11 @@ class TreeAttention:
                              "workspace")
         self.ws = tg.workspace(self.ws_bytes, q.device)
         self._ref, self._device, self._ws = ctypes.byref(a), q.get_device(), self.ws.data_ptr()
+        self._call = tg.load().tg_tree_attention
 
     def __call__(self, layer=0, stream=None):
         self.args.layer = layer
-        _check(tg.load().tg_tree_attention(self._ref, self._ws, self.ws_bytes,
-                                           _stream(stream, self._device)), "tg_tree_attention")
+        _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
         return self.out
 
 
@@ -307,9 +311,8 @@ class VerifyTree:
             raise tg.TgError(tg.load().tg_verify_tree(ctypes.byref(a), None, 0, None), "workspace")
         self.ws = tg.workspace(self.ws_bytes, target_probs.device)
         self._ref, self._device = ctypes.byref(a), target_probs.get_device()
-        self._ws = self.ws.data_ptr()
+        self._ws, self._call = self.ws.data_ptr(), tg.load().tg_verify_tree
 
     def __call__(self, stream=None):
-        _check(tg.load().tg_verify_tree(self._ref, self._ws, self.ws_bytes,
-                                        _stream(stream, self._device)), "tg_verify_tree")
+        _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
         return self.tokens_out, self.path, self.n_out

@@ -3,8 +3,9 @@ wrongly (CPU-only: checked on the host, before anything reaches the GPU)."""
 import ctypes
 
 import pytest
+import torch
 
-from paper_2601_01310_amd import tg
+from paper_2601_01310_amd import spec, tg
 from tests.test_spec_abi import attn_args, cache, lib  # noqa: F401 (a fixture)
 
 
@@ -33,3 +34,58 @@ def test_more_typical_rows_than_the_bound_change_nothing(lib, max_nodes):  # noq
         return lib.tg_tree_attention_workspace(ctypes.byref(
             attn_args(max_nodes=max_nodes, typical_nodes=typical)))
     assert need(0) == need(max_nodes) == need(1000) > 0
+
+
+class _Machine:
+    """Several devices, each with its streams, and a library that notes what
+    was current when it was called."""
+
+    def __init__(self, monkeypatch, current):
+        self.current, self.calls = current, []
+
+        class device:
+            def __init__(_, d):
+                _.d = d
+
+            def __enter__(_):
+                _.was, self.current = self.current, _.d
+
+            def __exit__(_, *exc):
+                self.current = _.was
+
+        class Lib:
+            def __getattr__(_, name):
+                def call(*args):
+                    self.calls.append((name, self.current, args[-1]))
+                    return tg.TG_OK
+                return call
+
+        self.lib = Lib()
+        monkeypatch.setattr(spec, "_current_device", lambda: self.current)
+        monkeypatch.setattr(spec, "_current_stream", lambda d: 1000 + d)
+        monkeypatch.setattr(torch.cuda, "device", device)
+        monkeypatch.setattr(spec, "_int32", lambda t, name, d, n, dim=1: 0)
+
+
+@pytest.mark.parametrize("current", [0, 1])
+@pytest.mark.parametrize("stream,raw", [(None, 1001), (0, 0), (77, 77)])
+def test_calls_run_on_the_device_of_their_tensors(monkeypatch, current, stream, raw):
+    """Whatever device is current: the null stream, which torch's default
+    stream is, belongs to the current one."""
+    m = _Machine(monkeypatch, current)
+    i = torch.zeros((3, 3), dtype=torch.int32)
+    c = spec.KvCache.__new__(spec.KvCache)
+    c.args, c._ref, c._device, c._lib = tg.KvCacheArgs(), None, 1, m.lib
+    c.reserve(i, i, i, i, stream=stream)
+    c.fork(i, i, i, i, stream=stream)
+    c.trim(i, stream=stream)
+    c.compact(i, i, i, i, stream=stream)
+    for kind in (spec.QkNormRope, spec.TreeAttention, spec.VerifyTree):
+        x = kind.__new__(kind)
+        x.args, x._ref, x._device, x._ws, x.ws_bytes = tg.QkArgs(), None, 1, 0, 0
+        x._call = m.lib.anything
+        x.q_out = x.out = x.tokens_out = x.path = x.n_out = i
+        x(stream=stream)
+    assert len(m.calls) == 7
+    assert {(d, s) for _, d, s in m.calls} == {(1, raw)}, m.calls
+    assert m.current == current
