@@ -452,15 +452,16 @@ tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
  *   out[r, h] = sum_p softmax_p(scale * q[r, h] . k[p, h / G]) * v[p, h / G]
  * over p in [0, lengths[b]) and lengths[b] + j for the nodes j seen, with
  * G = Hq / Hkv. Scores, the softmax's maximum and sum and the output's sums
- * are float32; probabilities are rounded to the cache's type for their
- * product with v. A row that sees nothing gives zeros. Positions that a row
- * does not see do not reach it, whatever they hold (infinities and NaN
- * included). max_nodes bounds the nodes per request (rows beyond it are not
- * written); positions beyond the page table are not there. typical_nodes is how
- * many rows most requests have, if max_nodes says little about it (0: max_nodes):
- * the kernel is chosen for it, any choice is right. The work is dealt evenly
- * over the device whatever the lengths; a request's last bits may depend on the
- * others of its batch, but not on the run. With G' = G / 16, the limit is
+ * are float32; probabilities are rounded to the cache's type for their product
+ * with v (in f16 to no finer step than 2^-31 of the largest). A row that sees
+ * nothing gives zeros. Positions that a row does not see do not reach it,
+ * whatever they hold (infinities and NaN included). max_nodes bounds the nodes
+ * per request (rows beyond it are not written); positions beyond the page
+ * table are not there. typical_nodes is how many rows most requests have, if
+ * max_nodes says little about it (0: max_nodes): the kernel is chosen for it,
+ * any choice is right. The work is dealt evenly over the device whatever the
+ * lengths; a request's last bits may depend on the others of its batch, but
+ * not on the run. With G' = G / 16, the limit is
  *   Hkv * min(B * (max_nodes * G' + 1), T * G' + B) * max_pages * page_size / 64
  *     < 2^30.
  */

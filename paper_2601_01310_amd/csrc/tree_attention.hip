@@ -5,9 +5,10 @@
 // share it) are the columns of two matrix products per 32 positions,
 //   S^T = K Q^T   and   O^T = V^T P^T,
 // with P = 2^(c S - m) between them (c = scale * log2 e, m a running maximum
-// per row). A lane holds, of S^T, exactly the positions that it feeds to the
-// second product, so P never leaves the registers, and the only operand that
-// needs a transpose is V, which comes out of LDS through ds_read_b64_tr_b16.
+// per row; 2^7 times that for f16). A lane holds, of S^T, exactly the positions
+// that it feeds to the second product, so P never leaves the registers, and the
+// only operand that needs a transpose is V, which comes out of LDS through
+// ds_read_b64_tr_b16.
 //
 // Few rows (split kernel): the cache's bytes bound it. A wave takes 32
 // positions at a time by itself, K straight from the cache into the operand's
@@ -61,17 +62,23 @@ __device__ __forceinline__ f32x4 mfma<F16>(const uint4& a, const uint4& b, f32x4
                                                 __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// The infinities and NaN of a pair of values, or (keep false) the pair without.
+// Of a type: the bits of the exponent that infinities and NaN have, and how many
+// powers of two probabilities are held above their value. f16 loses precision
+// below 2^-14 and all of it below 2^-25, where a long context after one large
+// score would vanish; bf16 has float32's range.
 template <class T>
 struct Exponent;
 template <>
 struct Exponent<Bf16> {
   static constexpr uint32_t kAll = 0x7f80u;
+  static constexpr float kUp = 0.0f;
 };
 template <>
 struct Exponent<F16> {
   static constexpr uint32_t kAll = 0x7c00u;
+  static constexpr float kUp = 7.0f;  // with kLazy 2^15 at most: below 65504
 };
+// The infinities and NaN of a pair of values, or (keep false) the pair without.
 template <class T>
 __device__ __forceinline__ uint32_t odd_part(uint32_t u, bool keep) {
   constexpr uint32_t e = Exponent<T>::kAll;
@@ -391,8 +398,9 @@ struct Rows {
   // Probabilities of kN / 2 tiles' scores, in the second product's layout:
   // element e of lane (quad, col) is position e / 4 * 16 + quad * 4 + e % 4 of
   // a tile. They are rounded to the cache's type (half a unit in the last
-  // place each, as much as the output's own rounding); the sum takes them
-  // unrounded.
+  // place each, as much as the output's own rounding; of f16, where that is
+  // more, 2^-32 of the largest); the sum takes them unrounded. Probabilities,
+  // their sum and o are 2^kUp times as large, which 1 / sum takes back.
   template <int kN>
   __device__ __forceinline__ void weigh(const f32x4 (&s)[kQ][kN], float scale,
                                         uint4 (&pr)[kN / 2][kQ]) {
@@ -411,7 +419,7 @@ struct Rows {
 #pragma unroll
         for (int d = 0; d < kCols; ++d) o[c][d] *= a;
       }
-      const float base = m[c] == -INFINITY ? 0.0f : m[c];
+      const float base = m[c] == -INFINITY ? 0.0f : m[c] - Exponent<T>::kUp;
 #pragma unroll
       for (int h = 0; h < kN / 2; ++h) {
         float e[8];

@@ -101,3 +101,42 @@ def test_a_long_request_among_short_ones_without_max_nodes(Hq, Hkv, D, dtype, pa
     for m in (mask, None):
         call = spec.TreeAttention(cache, q, torch.from_numpy(off).to(DEV), ints(L), m)
         check_attention(call(), f64(q), cache, table, 0, off, L, m, 1 / math.sqrt(D), dtype)
+
+
+@pytest.mark.parametrize("rows,Hq,D", [(1, 2, 64), (12, 4, 128), (40, 2, 64), (9, 4, 256)])
+def test_f16_keeps_a_long_context_behind_one_large_score(rows, Hq, D):
+    """The first token scores about 18 above all others, whose values alone
+    make the output: each of their probabilities is 2^-26 of the largest.
+
+    f16's subnormal step limits a probability to 2^-25 / 2^7 of the largest
+    score's: up to 2^-32 |v| for each position, over the sum of e^(s - max).
+    """
+    say(f"attention, f16 behind a large score, {rows} rows, D={D}")
+    rng = np.random.default_rng(rows)
+    L = 6000
+    k = torch.zeros((1, (L + rows + 63) // 64, 64, 1, D), dtype=torch.float16, device=DEV)
+    v = torch.zeros_like(k)
+    table = rng.permutation(k.shape[1]).astype(np.int32)[None]
+    at = torch.from_numpy(table[0].astype(np.int64)).to(DEV)
+    q = torch.randn((rows, Hq, D), device=DEV).half()
+    q[..., 0] = 4.0
+    K = torch.randn((k.shape[1] * 64, D), device=DEV) * 0.1
+    V = 1 + 0.5 * torch.randn((k.shape[1] * 64, D), device=DEV)
+    K[:, 0] = 0
+    K[0], V[0] = 0, 0
+    K[0, 0] = 18 * math.sqrt(D) / 4
+    k[0, at, :, 0], v[0, at, :, 0] = K.half().view(-1, 64, D), V.half().view(-1, 64, D)
+    ones = torch.ones(k.shape[1], dtype=torch.int32, device=DEV)
+    cache = spec.KvCache(k, v, torch.from_numpy(table).to(DEV), ints([k.shape[1]]), ones)
+    got = f64(spec.TreeAttention(cache, q, ints([0, rows]), ints([L]))())
+    hk, hv, hq = f64(k[0, at].flatten(0, 1)[:, 0]), f64(v[0, at].flatten(0, 1)[:, 0]), f64(q)
+    for r in range(rows):
+        n = L + r + 1
+        for h in range(Hq):
+            s = hk[:n] @ hq[r, h] / math.sqrt(D)
+            p = np.exp(s - s.max())
+            ref, size = p @ hv[:n] / p.sum(), p @ np.abs(hv[:n]) / p.sum()
+            tol = (2.0 ** -11 * (size * (1 + 1 / 16) + np.abs(ref)) + 2.0 ** -25
+                   + 2.0 ** -32 * np.abs(hv[:n]).sum(0) / p.sum())
+            assert s[0] - s[1:].max() > 17 and ref.min() > 20 * tol.max()
+            assert (np.abs(got[r, h] - ref) <= tol).all(), (r, h, got[r, h][:4], ref[:4], tol[:4])
