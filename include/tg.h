@@ -504,7 +504,9 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
  * with one token the second is not. Rows sum to about 1 (beyond 2^17 the sums
  * are no longer exact and some token of the row comes out).
  * At most max_path nodes are kept, the root among them: deeper ones are
- * ignored. Outputs, for request b: n_out[b] = kept nodes (0 if it has no
+ * ignored. status (tg_kv_pages_reserve's, or NULL): a request whose status is 0
+ * has no K and V of its nodes in the cache and keeps nothing, like one without
+ * rows. Outputs, for request b: n_out[b] = kept nodes (0 if it has no
  * rows), path [B, max_path] their numbers in order (0 first, then -1),
  * tokens_out [B, max_path] the tokens after each of them: the drafted ones
  * kept, then the one drawn (then -1).
@@ -522,6 +524,7 @@ typedef struct {
   int32_t* tokens_out;
   int32_t* path;
   int32_t* n_out;
+  const int32_t* status; /* [B] or NULL */
 } tg_verify_args;
 
 size_t tg_verify_tree_workspace(const tg_verify_args* a);
@@ -543,7 +546,8 @@ tg_status tg_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
  * q_offsets[b+1] - q_offsets[b] tokens, in request order and the lowest free
  * page first; from the first request on for which too few pages are free, none
  * that needs pages gets any, and a request whose row of the table is too short
- * gets and takes none (status[b] 0 instead of 1). slots [T] is where each new
+ * gets and takes none (status[b] 0 instead of 1: its rows are not cached, and
+ * tg_verify_tree is told so). slots [T] is where each new
  * row goes in the cache (page * page_size + row), -1 where its request got no
  * pages. A request may already hold the pages that it needs.
  *

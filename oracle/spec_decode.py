@@ -163,12 +163,14 @@ def verify_request(p, q, tokens, u_accept, u_next, masks, max_path) -> Dict[str,
     return dict(path=path, tokens=out + [0 if x is None else x])
 
 
-def verify(p, q, tokens, u_accept, u_next, q_offsets, tree_mask, max_path):
+def verify(p, q, tokens, u_accept, u_next, q_offsets, tree_mask, max_path, status=None):
     """(tokens_out [B, max_path], path [B, max_path], n_out [B])."""
     B = len(u_next)
     tok, path = (np.full((B, max_path), -1, np.int32) for _ in range(2))
     n_out = np.zeros(B, np.int32)
     for b in range(B):
+        if status is not None and status[b] == 0:
+            continue
         s = slice(q_offsets[b], q_offsets[b + 1])
         masks = None if tree_mask is None else [mask_bits(m) for m in tree_mask[s]]
         r = verify_request(p[s], None if q is None else q[s], tokens[s], u_accept[s], u_next[b],

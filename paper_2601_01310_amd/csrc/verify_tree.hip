@@ -119,7 +119,7 @@ __device__ __forceinline__ double drawn_mass(uint64_t u, double mass) {
 
 // What the walk leaves for the draw of a request.
 struct Drawn {
-  int row, use_q, n_drop, kept;  // kept 0: the request has no rows
+  int row, use_q, n_drop, kept;  // kept 0: the request has no rows, or no pages
 };
 
 struct Space {
@@ -147,6 +147,7 @@ __global__ __launch_bounds__(kBlock) void walk_kernel(const tg_verify_args a, in
   const bool writes = part == 0;
   int first, n;
   request_rows(a.q_offsets, b, a.T, a.max_nodes, &first, &n);
+  if (a.status && a.status[b] == 0) n = 0;
   int32_t* const path = a.path + (int64_t)b * a.max_path;
   int32_t* const out = a.tokens_out + (int64_t)b * a.max_path;
   if (writes)

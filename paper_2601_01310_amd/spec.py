@@ -271,11 +271,13 @@ class TreeAttention:
 class VerifyTree:
     """Which drafted tokens stay. ``target_probs`` (and ``draft_probs``) [T, V]
     float32 with dense rows, ``tokens`` [T] int32, ``u_accept`` [T] and
-    ``u_next`` [B] float32 in [0, 1). Returns (tokens_out [B, max_path], path
+    ``u_next`` [B] float32 in [0, 1). ``status`` [B] int32: that of
+    :meth:`KvCache.reserve`, whose refused requests keep nothing (without it, give
+    only requests that have got their pages). Returns (tokens_out [B, max_path], path
     [B, max_path], n_out [B]) int32."""
 
     def __init__(self, target_probs, tokens, u_accept, u_next, q_offsets, tree_mask=None,
-                 max_path=None, max_nodes=None, draft_probs=None):
+                 max_path=None, max_nodes=None, draft_probs=None, status=None):
         T, V = target_probs.shape
         B = u_next.shape[0]
         stride = _rows(target_probs, "target_probs", torch.float32, (V,))
@@ -288,8 +290,10 @@ class VerifyTree:
         _want(u_accept, "u_accept", torch.float32, (T,))
         _want(u_next, "u_next", torch.float32, (B,))
         _want(q_offsets, "q_offsets", torch.int32, (B + 1,))
+        _want(status, "status", torch.int32, (B,), optional=True)
         words = _mask(tree_mask, T)
-        _same_device(target_probs, draft_probs, tokens, u_accept, u_next, q_offsets, tree_mask)
+        _same_device(target_probs, draft_probs, tokens, u_accept, u_next, q_offsets, tree_mask,
+                     status)
         if max_nodes is None:
             max_nodes = max(1, min(T, tg.MAX_NODES, 64 * words if words else tg.MAX_NODES))
         max_path = max_nodes if max_path is None else max_path
@@ -297,14 +301,15 @@ class VerifyTree:
         self.tokens_out = torch.empty((B, max_path), **ints)
         self.path = torch.empty((B, max_path), **ints)
         self.n_out = torch.empty((B,), **ints)
-        self._keep = (target_probs, draft_probs, tokens, u_accept, u_next, q_offsets, tree_mask)
+        self._keep = (target_probs, draft_probs, tokens, u_accept, u_next, q_offsets, tree_mask,
+                      status)
         a = self.args = tg.VerifyArgs()
         a.B, a.T, a.V, a.max_path, a.max_nodes, a.mask_words = B, T, V, max_path, max_nodes, words
         a.target_stride, a.draft_stride = stride, draft_stride
         for name, t in dict(target_probs=target_probs, draft_probs=draft_probs, tokens=tokens,
                             u_accept=u_accept, u_next=u_next, q_offsets=q_offsets,
                             tree_mask=tree_mask, tokens_out=self.tokens_out, path=self.path,
-                            n_out=self.n_out).items():
+                            n_out=self.n_out, status=status).items():
             setattr(a, name, None if t is None else t.data_ptr())
         self.ws_bytes = tg.tg_verify_tree_workspace(a)
         if self.ws_bytes == 0:

@@ -91,7 +91,7 @@ class VerifyArgs(ctypes.Structure):
     _fields_ = _fields([
         ("int", "B T V max_path max_nodes mask_words"), ("i64", "target_stride draft_stride"),
         ("ptr", "target_probs draft_probs tokens u_accept u_next q_offsets tree_mask tokens_out "
-                "path n_out")])
+                "path n_out status")])
 
 
 BF16, F16 = 0, 1

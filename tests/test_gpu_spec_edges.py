@@ -7,9 +7,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import spec_decode as S
 from paper_2601_01310_amd import spec
 from tests.test_gpu_spec_decode import (DEV, check_attention, f64, ints, make_pool, random_masks,
-                                        say)
+                                        say, verify_inputs)
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +141,38 @@ def test_f16_keeps_a_long_context_behind_one_large_score(rows, Hq, D):
                    + 2.0 ** -32 * np.abs(hv[:n]).sum(0) / p.sum())
             assert s[0] - s[1:].max() > 17 and ref.min() > 20 * tol.max()
             assert (np.abs(got[r, h] - ref) <= tol).all(), (r, h, got[r, h][:4], ref[:4], tol[:4])
+
+
+@pytest.mark.parametrize("sampled", [False, True])
+def test_requests_without_pages_keep_nothing(sampled):
+    """Pages for two of three requests: the third one's rows are not cached, so
+    it keeps none of them, and its length stays until it gets pages."""
+    say(f"verify with a status, sampled={sampled}")
+    n, V, page = 6, 500, 4
+    cache = spec.KvCache.empty(1, 4, page, 1, 64, 3, 3, device=DEV)
+    lengths, new, off = ints([0, 0, 0]), ints([-1] * 3), ints([0, n, 2 * n, 3 * n])
+    slots, status = ints([9] * 3 * n), ints([9] * 3)
+    p, q, mask, off_h, tokens, u, un = verify_inputs([n] * 3, V, sampled, 5)
+    p.zero_()
+    p[:, 7] = 1.0
+    tokens[:] = 7  # every draft would stay
+    if sampled:
+        q.copy_(p)
+    say("  reserve, verify, compact")
+    check = spec.VerifyTree(p, *(torch.from_numpy(x).to(DEV) for x in (tokens, u, un)), off, mask,
+                            max_path=n, draft_probs=q, status=status)
+    cache.reserve(lengths, off, slots, status)
+    assert status.tolist() == [1, 1, 0] and set(slots.tolist()[2 * n:]) == {-1}
+    got = [x.cpu().numpy() for x in check()]
+    ref = S.verify(p.cpu().numpy(), None if q is None else q.cpu().numpy(), tokens, u, un, off_h,
+                   None if mask is None else mask.cpu().numpy().view(np.uint64), n, [1, 1, 0])
+    for a, b in zip(got, ref):
+        assert np.array_equal(a, b)
+    assert got[2].tolist()[0] > 1 and got[2].tolist()[2] == 0
+    cache.compact(check.path, check.n_out, lengths, new)
+    assert new.tolist() == got[2].tolist()
+    cache.trim(ints([0, 0, 0]))
+    cache.reserve(lengths, off, slots, status)  # all pages free: still two of three
+    assert status.tolist() == [1, 1, 0]
+    status.copy_(ints([0, 1, 1]))
+    assert check()[2].tolist()[0] == 0
