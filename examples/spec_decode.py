@@ -48,9 +48,12 @@ def rms(x):
 
 
 class Worker:
-    """A batch of B requests, up to T rows per forward."""
+    """A batch of B requests, up to T rows per forward and ``max_tokens`` in the
+    cache per request, those of the rows in flight included."""
 
     def __init__(self, w, B, T, max_tokens=256, device="cuda"):
+        if max_tokens > w["cos_sin"].shape[0]:
+            raise ValueError(f"{max_tokens} tokens: angles for {w['cos_sin'].shape[0]} only")
         ints = dict(dtype=torch.int32, device=device)
         self.w, self.B, self.T = w, B, T
         width = -(-max_tokens // PAGE) + 1
@@ -66,6 +69,8 @@ class Worker:
                                      w["norm"][2 * i], w["norm"][2 * i + 1]) for i in range(LAYERS)]
         self.attend = [spec.TreeAttention(self.cache, r.q_out, self.offsets, self.lengths,
                                           self.mask) for r in self.rope]
+        for a in self.attend:
+            a.out.zero_()  # rows that no request has are not written
         self.experts = [tg.EwForward(synth.make_custom(
             T=T, d=D_MODEL, E=8, k=2, I=512, n_local=8, shadow_experts=[0], gate="weights",
             seed=50 + i, device=device)) for i in range(LAYERS)]
@@ -75,6 +80,8 @@ class Worker:
         positions describe; their K and V are in the cache afterwards."""
         w = self.w
         self.cache.reserve(self.lengths, self.offsets, self.slots, self.status)
+        if not self.status.all():
+            raise RuntimeError("the cache has no pages for these rows")
         x = w["embed"][self.tokens.long()].float()
         for i in range(LAYERS):
             torch.mm(rms(x), w["qkv"][i], out=self.qkv.view(self.T, -1))
@@ -112,10 +119,16 @@ class Worker:
             self.lengths += torch.diff(self.offsets)
 
 
+def room(prompts, n, nodes):
+    """Cached tokens that a request of the batch may need: a request ends with
+    its n-th token, which a step may pass by the nodes of a tree."""
+    return max(256, max(map(len, prompts)) + n + nodes)
+
+
 def greedy(w, prompts, n):
     """n tokens of each request, one forward per token."""
     B = len(prompts)
-    worker = Worker(w, B, B)
+    worker = Worker(w, B, B, room(prompts, n, 1))
     worker.prefill(prompts)
     last, out = [p[-1] for p in prompts], [[] for _ in prompts]
     for _ in range(n):
@@ -131,7 +144,7 @@ def speculative(w, prompts, n, store=None):
     """The same tokens from drafted trees; returns them and the forwards
     needed. ``store``: a pinned host copy of the K pages to checkpoint into."""
     B, N = len(prompts), len(TREE)
-    worker = Worker(w, B, B * N)
+    worker = Worker(w, B, B * N, room(prompts, n, N))
     worker.prefill(prompts)
     masks, depths = [1], [0]
     for j, (up, _) in enumerate(TREE[1:], 1):
@@ -142,7 +155,7 @@ def speculative(w, prompts, n, store=None):
     probs = torch.zeros((B * N, VOCAB), device="cuda")
     zeros = torch.zeros(B * N, device="cuda")
     check = spec.VerifyTree(probs, worker.tokens, zeros, zeros[:B], worker.offsets, worker.mask,
-                            max_path=N)
+                            max_path=N, status=worker.status)
     last, out, steps, seq = [p[-1] for p in prompts], [[] for _ in prompts], 0, 1
     while min(len(o) for o in out) < n:
         tokens = []
@@ -151,7 +164,9 @@ def speculative(w, prompts, n, store=None):
             for up, which in TREE[1:]:
                 t.append(int(draft[t[up], which]))
             tokens.append(t)
-        worker.rows(tokens, [masks] * B, [depths] * B)
+        going = [len(o) < n for o in out]  # a request ends with its n-th token
+        worker.rows(*([x if on else [] for x, on in zip(rows, going)]
+                      for rows in (tokens, [masks] * B, [depths] * B)))
         logits = worker.forward()
         probs.zero_().scatter_(1, logits.argmax(1, keepdim=True), 1.0)  # greedy: all mass on one
         new, path, kept = check()
@@ -162,8 +177,9 @@ def speculative(w, prompts, n, store=None):
         worker.cache.trim(worker.lengths)  # pages of refused rows
         steps += 1
         for b, (row, k) in enumerate(zip(new.tolist(), kept.tolist())):
-            out[b] += row[:k]
-            last[b] = row[k - 1]
+            if k:
+                out[b] += row[:k]
+                last[b] = row[k - 1]
     return [o[:n] for o in out], steps, worker
 
 

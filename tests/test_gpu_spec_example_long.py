@@ -1,0 +1,35 @@
+"""The example's decoder beyond the sizes of its first test: it has room for the
+tokens that are asked for, and stops where it has none."""
+import pytest
+import torch
+
+from tests.test_gpu_spec_example import ex  # noqa: F401 (a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def test_long_answers_have_their_pages(ex):  # noqa: F811
+    print("[gpu] speculative decoding, 300 tokens of 3 requests", flush=True)
+    prompts = [[1, 2, 3], [9] * 40, [5]]
+    tokens, steps, worker = ex.speculative(ex.weights("cuda"), prompts, 300)
+    assert [len(t) for t in tokens] == [300] * 3 and steps <= 300
+    L = worker.lengths.tolist()
+    for p, n in zip(prompts, L):  # the last step may pass the 300th token
+        assert len(p) - 1 + 300 <= n < len(p) - 1 + 300 + len(ex.TREE)
+    held = [-(-n // ex.PAGE) for n in L]
+    assert worker.cache.held.tolist() == held and int(worker.cache.refcount.sum()) == sum(held)
+
+
+def test_a_worker_without_pages_says_so(ex):  # noqa: F811
+    print("[gpu] a worker that runs out of pages", flush=True)
+    w = ex.weights("cuda")
+    worker = ex.Worker(w, 1, 4, max_tokens=ex.PAGE)
+    room = worker.cache.page_table.shape[1] * ex.PAGE
+    worker.prefill([[1] * (room + 1)])  # the last token is not cached
+    assert worker.lengths.tolist() == [room]
+    worker.rows([[1]], [[1]], [[0]])
+    with pytest.raises(RuntimeError, match="no pages"):
+        worker.forward()
+    with pytest.raises(ValueError, match="angles"):
+        ex.Worker(w, 1, 1, max_tokens=1 << 20)
+    torch.cuda.synchronize()
