@@ -409,7 +409,7 @@ hipError_t launch_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_
 hipError_t launch_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
                                    const int32_t* q_offsets, int T, int32_t* slots, int32_t* status,
                                    hipStream_t s) {
-  if (c->B == 0) return hipSuccess;
+  if (c->B == 0 && T == 0) return hipSuccess;  // T rows of nobody still get their -1
   hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kBlock), 0, s, c->page_table, c->held,
                      c->refcount, c->n_pages, __builtin_ctz(c->page_size), c->B, c->max_pages,
                      lengths, q_offsets, T, slots, status, static_cast<uint16_t*>(c->k),

@@ -176,3 +176,14 @@ def test_requests_without_pages_keep_nothing(sampled):
     assert status.tolist() == [1, 1, 0]
     status.copy_(ints([0, 1, 1]))
     assert check()[2].tolist()[0] == 0
+
+
+def test_a_batch_without_requests_gets_no_slots():
+    """Slots kept from another batch must not lead rows into the cache."""
+    say("reserve without requests")
+    cache = spec.KvCache.empty(1, 4, 16, 1, 64, 0, 2, device=DEV)
+    slots = ints([5] * 70)
+    cache.reserve(ints([]), ints([0]), slots, ints([]))
+    assert slots.tolist() == [-1] * 70
+    cache.reserve(ints([]), ints([0]), slots[:0], ints([]))
+    assert cache.refcount.tolist() == [0] * 4

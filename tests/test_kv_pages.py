@@ -144,3 +144,13 @@ def test_sequences_with_rollbacks(lib, B, size, n_pages, width, seed):
         lengths = np.maximum(lengths - back, 0).astype(np.int32)
         if step % 2:
             c.oracle.trim(lengths)
+
+
+def test_rows_of_no_request_get_no_slots(lib):
+    for B, T in ((0, 70), (2, 70)):
+        off, slots, status = np.zeros(B + 1, np.int32), np.full(T, 5, np.int32), np.zeros(2, np.int32)
+        table, held, refs = np.full((2, 2), -1, np.int32), np.zeros(2, np.int32), np.zeros(4, np.int32)
+        rows = np.zeros((1, 4, 16, 64), np.uint16)
+        lib.reserve(_p(table), _p(held), _p(refs), 4, 4, B, 2, _p(held), _p(off), T, _p(slots),
+                    _p(status), _p(rows), _p(rows), 1, 64)
+        assert (slots == -1).all() and (refs == 0).all()
