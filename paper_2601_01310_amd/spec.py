@@ -45,7 +45,8 @@ def _want(t: Optional[torch.Tensor], name: str, dtype, shape=None, optional=Fals
 
 
 def _rows(t: torch.Tensor, name: str, dtype, inner) -> int:
-    """Checks [rows, *inner] with dense rows; returns the row stride."""
+    """Checks [rows, *inner] with dense rows; returns the row stride (of one row,
+    whose stride means nothing, one that is taken)."""
     if t.device.type != "cuda":
         raise ValueError(f"{name}: libtg takes device tensors only")
     if t.dtype != dtype:
@@ -57,7 +58,7 @@ def _rows(t: torch.Tensor, name: str, dtype, inner) -> int:
         if n > 1 and stride != dense:
             raise ValueError(f"{name}: a row must be contiguous")
         dense *= n
-    return t.stride(0) if t.shape[0] > 1 else max(dense, t.stride(0))
+    return t.stride(0) if t.shape[0] > 1 else -(-max(dense, t.stride(0)) // 8) * 8
 
 
 _current_device = torch._C._cuda_getDevice

@@ -187,3 +187,20 @@ def test_a_batch_without_requests_gets_no_slots():
     assert slots.tolist() == [-1] * 70
     cache.reserve(ints([]), ints([0]), slots[:0], ints([]))
     assert cache.refcount.tolist() == [0] * 4
+
+
+def test_one_row_may_come_with_any_stride():
+    """A slice of one row keeps the stride of what it was cut from."""
+    say("one row, odd strides")
+    rng = np.random.default_rng(12)
+    cache, table = make_pool([40], 16, 1, 64, torch.bfloat16, rng)
+    wide = torch.randn((1, 4 * 64 + 3), device=DEV).to(torch.bfloat16)
+    q = torch.as_strided(wide, (1, 4, 64), (4 * 64 + 3, 64, 1))
+    off, L = ints([0, 1]), ints([39])
+    a = spec.TreeAttention(cache, q, off, L)()
+    assert torch.equal(a, spec.TreeAttention(cache, q.contiguous().view(1, 4, 64), off, L)())
+    qkv = torch.as_strided(wide, (1, 4, 64), (4 * 64 + 3, 64, 1))
+    slots, w = ints([39]), torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    want = spec.QkNormRope(cache, qkv, 2, None, slots, None, w, w)().clone()
+    spec.QkNormRope(cache, qkv, 2, None, slots, None, w, w, q_out=qkv[:, :2])()  # in place
+    assert torch.equal(qkv[:, :2], want)
