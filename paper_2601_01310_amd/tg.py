@@ -329,46 +329,12 @@ def tg_kv_restore(store, store_bytes, commit, seq, src, dst, nbytes, n, kv_dst, 
                                 _stream(stream)), "tg_kv_restore")
 
 
-def tg_qk_norm_rope(args: QkArgs, stream=None):
-    _check(load().tg_qk_norm_rope(ctypes.byref(args), _stream(stream)), "tg_qk_norm_rope")
-
-
 def tg_tree_attention_workspace(args: TreeAttnArgs) -> int:
     return int(load().tg_tree_attention_workspace(ctypes.byref(args)))
 
 
-def tg_tree_attention(args: TreeAttnArgs, ws, ws_bytes, stream=None):
-    _check(load().tg_tree_attention(ctypes.byref(args), _p(ws), ws_bytes, _stream(stream)),
-           "tg_tree_attention")
-
-
 def tg_verify_tree_workspace(args: VerifyArgs) -> int:
     return int(load().tg_verify_tree_workspace(ctypes.byref(args)))
-
-
-def tg_verify_tree(args: VerifyArgs, ws, ws_bytes, stream=None):
-    _check(load().tg_verify_tree(ctypes.byref(args), _p(ws), ws_bytes, _stream(stream)),
-           "tg_verify_tree")
-
-
-def tg_kv_compact(cache: KvCacheArgs, path, max_path, n_keep, lengths, new_lengths, stream=None):
-    _check(load().tg_kv_compact(ctypes.byref(cache), _p(path), max_path, _p(n_keep), _p(lengths),
-                                _p(new_lengths), _stream(stream)), "tg_kv_compact")
-
-
-def tg_kv_pages_reserve(cache: KvCacheArgs, lengths, q_offsets, T, slots, status, stream=None):
-    _check(load().tg_kv_pages_reserve(ctypes.byref(cache), _p(lengths), _p(q_offsets), T, _p(slots),
-                                      _p(status), _stream(stream)), "tg_kv_pages_reserve")
-
-
-def tg_kv_pages_fork(cache: KvCacheArgs, lengths, src, dst, n, status, stream=None):
-    _check(load().tg_kv_pages_fork(ctypes.byref(cache), _p(lengths), _p(src), _p(dst), n,
-                                   _p(status), _stream(stream)), "tg_kv_pages_fork")
-
-
-def tg_kv_pages_trim(cache: KvCacheArgs, keep, stream=None):
-    _check(load().tg_kv_pages_trim(ctypes.byref(cache), _p(keep), _stream(stream)),
-           "tg_kv_pages_trim")
 
 
 def _flag_ptr(t):
