@@ -130,9 +130,14 @@ template <class T, int D>
 hipError_t launch(const tg_qk_args* a, hipStream_t s) {
   const tg_kv_cache& c = a->cache;
   const int heads = a->Hq + 2 * c.Hkv, per = kWave / (D / 8);
-  // Few rows: one pass of a wave's lane groups over kU heads each, so that
-  // all heads are in flight at once; many rows: a wave takes a whole row.
-  const int heads_per_wave = a->T >= 1024 ? heads : per * kU;
+  // Few rows: one pass of a wave's lane groups over kU heads each, so that all
+  // heads are in flight at once. Many rows fill the device without, and a wave
+  // takes a whole row, loading its angles once. A wave per row against a pass
+  // per wave, in us: 48 heads of 128, 1024 rows 9.9 / 7.2, 2048 rows 13.0 /
+  // 12.3, 3000 rows 15.3 / 16.2, 8192 rows 34.6 / 34.9; 12 heads of 256, 1024
+  // rows 7.5 / 5.6, 2048 rows 8.8 / 8.0, 3000 rows 10.7 / 11.5, 8192 rows
+  // 21.3 / 22.7. (32 heads of 64 are one pass either way.)
+  const int heads_per_wave = a->T >= 2560 ? heads : per * kU;
   const dim3 grid((a->T + kBlock / kWave - 1) / (kBlock / kWave),
                   (heads + heads_per_wave - 1) / heads_per_wave);
   auto go = [&](auto kernel) {

@@ -204,3 +204,26 @@ def test_one_row_may_come_with_any_stride():
     want = spec.QkNormRope(cache, qkv, 2, None, slots, None, w, w)().clone()
     spec.QkNormRope(cache, qkv, 2, None, slots, None, w, w, q_out=qkv[:, :2])()  # in place
     assert torch.equal(qkv[:, :2], want)
+
+
+def test_norms_and_rotation_either_side_of_the_choice_of_grid():
+    """A row takes a wave or several, by the number of rows: the same bits."""
+    say("qk, 2559 to 2561 rows of 20 heads")
+    rng = np.random.default_rng(13)
+    T, D = 2561, 128
+    cache, _ = make_pool([1], 16, 4, D, torch.bfloat16, rng, spare=T // 16 + 1, fill=0.0)
+    qkv = torch.randn((T, 20, D), device=DEV).to(torch.bfloat16)
+    w = torch.randn((2, D), device=DEV).to(torch.bfloat16)
+    t = torch.randn((T, D), device=DEV)
+    pos, slots = ints(rng.permutation(T).tolist()), ints(rng.permutation(T).tolist())
+    got = []
+    for n in (T, T - 1, T - 2, 7):
+        for x in (cache.k, cache.v):
+            x.zero_()
+        q = spec.QkNormRope(cache, qkv[:n], 12, pos[:n], slots[:n], t, *w)()
+        k, v = (x[0].flatten(0, 1)[slots.long()] for x in (cache.k, cache.v))
+        got.append((n, q, k, v))
+    for n, *parts in got[1:]:
+        for a, b in zip(parts, got[0][1:]):
+            assert torch.equal(a[:n], b[:n]), n
+            assert (a[n:] == 0).all()
