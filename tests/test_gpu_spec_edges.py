@@ -227,3 +227,68 @@ def test_norms_and_rotation_either_side_of_the_choice_of_grid():
         for a, b in zip(parts, got[0][1:]):
             assert torch.equal(a[:n], b[:n]), n
             assert (a[n:] == 0).all()
+
+
+@pytest.mark.parametrize("nodes,Hq,D,dtype", [
+    (1, 4, 128, torch.bfloat16), (40, 2, 64, torch.float16), (40, 2, 128, torch.bfloat16),
+    (40, 1, 256, torch.bfloat16), (1, 4, 256, torch.float16)])
+def test_the_most_requests_of_a_batch(nodes, Hq, D, dtype):
+    """4096 requests: the sums of their work take their whole place in LDS."""
+    say(f"attention, 4096 requests, kernel of {nodes} rows, D={D}")
+    rng = np.random.default_rng(D + nodes)
+    B, page = 4096, 4
+    L = rng.integers(0, 4, B)
+    L[[5, 4095]] = 130
+    N = rng.integers(0, 3, B)
+    N[[5, 4095]] = nodes
+    held = -(-(L + N) // page)
+    table = np.full((B, int(held.max())), -1, np.int32)
+    order = rng.permutation(int(held.sum())).astype(np.int32)
+    for b, at in enumerate(np.cumsum(held) - held):
+        table[b, :held[b]] = order[at:at + held[b]]
+    k, v = (torch.randn((1, len(order), page, 1, D), device=DEV).to(dtype) for _ in range(2))
+    cache = spec.KvCache(k, v, torch.from_numpy(table).to(DEV), ints(held.tolist()),
+                         torch.ones(len(order), dtype=torch.int32, device=DEV))
+    off = np.concatenate([[0], np.cumsum(N)]).astype(np.int32)
+    q = torch.randn((int(off[-1]), Hq, D), device=DEV).to(dtype)
+    out = spec.TreeAttention(cache, q, torch.from_numpy(off).to(DEV), ints(L.tolist()),
+                             max_nodes=max(nodes, 2))()
+    some = sorted({0, 5, 63, 64, 4095, *rng.integers(0, B, 60).tolist()})
+    rows = np.concatenate([np.arange(off[b], off[b + 1]) for b in some])
+    part = np.concatenate([[0], np.cumsum(N[some])]).astype(np.int32)
+    check_attention(out[rows], f64(q[rows]), cache, table[some], 0, part, L[some], None,
+                    1 / math.sqrt(D), dtype)
+
+
+@pytest.mark.parametrize("Hq,D,dtype,page,masked,L", [
+    (2, 128, torch.bfloat16, 16, False, 70), (1, 64, torch.float16, 64, True, 0),
+    (1, 256, torch.bfloat16, 32, True, 33)])
+def test_the_most_rows_of_a_request(Hq, D, dtype, page, masked, L):
+    """A prompt's chunk of 1024 rows, and one row more, which is not written."""
+    say(f"attention, 1024 rows, D={D} masked={masked}")
+    rng = np.random.default_rng(D)
+    n = 1024
+    cache, table = make_pool([L + n], page, 1, D, dtype, rng)
+    q = torch.randn((n + 1, Hq, D), device=DEV).to(dtype)
+    mask = random_masks([n + 1], rng, words=17)[:, :16].contiguous() if masked else None
+    out = torch.full((n + 1, Hq, D), 3.0, dtype=dtype, device=DEV)
+    spec.TreeAttention(cache, q, ints([0, n + 1]), ints([L]), mask, out=out)()
+    assert (out[n] == 3.0).all()
+    check_attention(out[:n], f64(q[:n]), cache, table, 0, [0, n], [L],
+                    None if mask is None else mask[:n], 1 / math.sqrt(D), dtype)
+
+
+@pytest.mark.parametrize("sampled", [False, True])
+def test_verification_of_the_most_nodes(sampled):
+    say(f"verify 1024 nodes, sampled={sampled}")
+    for seed in range(3):
+        p, q, mask, off, tokens, u, un = verify_inputs([1024, 3], 40, sampled, seed)
+        u *= 0.05  # long paths
+        u[1] = 0.0
+        call = spec.VerifyTree(p, *(torch.from_numpy(x).to(DEV) for x in (tokens, u, un, off)),
+                               tree_mask=mask, max_path=1024, draft_probs=q)
+        got = [t.cpu().numpy() for t in call()]
+        ref = S.verify(p.cpu().numpy(), None if q is None else q.cpu().numpy(), tokens, u, un, off,
+                       None if mask is None else mask.cpu().numpy().view(np.uint64), 1024)
+        for a, b in zip(got, ref):
+            assert np.array_equal(a, b), seed
