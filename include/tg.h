@@ -459,9 +459,9 @@ tg_status tg_qk_norm_rope(const tg_qk_args* a, void* stream);
  * per request (rows beyond it are not written); positions beyond the page
  * table are not there. typical_nodes is how many rows most requests have, if
  * max_nodes says little about it (0: max_nodes): the kernel is chosen for it,
- * any choice is right. The work is dealt evenly over the device whatever the
- * lengths; a request's last bits may depend on the others of its batch, but
- * not on the run. With G' = G / 16, the limit is
+ * any choice is right. The work is dealt to the device's blocks in runs of one
+ * length whatever the requests' lengths; a request's last bits may depend on
+ * the others of its batch, but not on the run. With G' = G / 16, the limit is
  *   Hkv * min(B * (max_nodes * G' + 1), T * G' + B) * max_pages * page_size / 64
  *     < 2^30.
  */
@@ -556,7 +556,8 @@ tg_status tg_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
  * new rows would lie in are then replaced by fresh ones (they count as pages
  * needed, before the new ones), with the tokens in use copied in every layer,
  * and the request's references to the old ones drop. The reference counts
- * before the call decide which pages are shared.
+ * before the call decide which pages are shared. (What is copied is new to a
+ * store that tg_kv_checkpoint keeps, here and in tg_kv_pages_fork.)
  */
 tg_status tg_kv_pages_reserve(const tg_kv_cache* c, const int32_t* lengths,
                               const int32_t* q_offsets, int T, int32_t* slots, int32_t* status,

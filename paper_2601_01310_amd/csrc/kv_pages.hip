@@ -5,13 +5,14 @@
 // that pages go out in a fixed order: a prefix sum of the pages that each
 // request (or fork) needs, one pass over the reference counts that deals the
 // free pages out in ascending order and stops with the last one needed, and
-// a last step that takes back what went to requests that did not fit: 4 to 10
+// a last step that takes back what went to requests that did not fit: 3 to 9
 // us a call, a handful of dependent loads (64 requests, 8000 pages). The bytes
 // (compaction, part pages of forks) move in kernels of their own over many
 // blocks, every row read and written once: 29 us for 17 400 pieces of 2 KB in
 // 32 layers and 14 us for 1024 part pages of up to 30 KB, both 2.5 TB/s read
-// and written. More in flight change little (64 layers: 2.8 TB/s): pieces of
-// 2 KB all over the memory, not the kernel, set that rate.
+// and written, whatever the pieces' size. What sets that rate is not shown; the
+// compiler keeps the pieces in flight in scratch memory (144 bytes a lane of
+// either kernel) instead of registers, which comes first in question.
 #include "tg_kv.h"
 
 namespace tg {

@@ -17,20 +17,22 @@
 // maxima, sums and outputs. 128 single tokens over contexts of up to 8192
 // (heads 32 / 8 of 128): 436 us, 5.6 TB/s; two waves per SIMD without spilled
 // registers are faster than three with (640 us). 7 rows over 131071 positions:
-// 113 us, 4.8 TB/s (blocks get 16 or 17 units: 6 % of them idle at the end).
+// 111 us, 4.8 TB/s (482 of the 512 blocks get 17 units, one 6, 29 none).
 // Many rows (shared kernel): the products and the vector unit bound it. The
 // four waves of a block take different rows and share each tile of 64
 // positions through LDS, which the split kernel would read per wave. Eight
 // trees of up to 64 rows over up to 16384 positions (heads 64 / 8 of 128):
-// 185 us, 600 TFLOP/s; the matrix unit works in 35 % of the time, the vector
-// unit (exp, maxima, conversions) in 44 %, LDS in 18 % without bank conflicts,
-// and a wave, of which two fit a SIMD, waits in 42 %.
+// 215 us on average of 30 traced launches and 185 at best, 520 to 600 TFLOP/s
+// (196 us with the join, among other calls); the matrix unit works in 35 % of the
+// time, the vector unit (exp, maxima, conversions) in 44 %, LDS in 18 % without
+// bank conflicts, and a wave, of which two fit a SIMD, waits in 42 %.
 //
-// The work is dealt evenly whatever the lengths: all (request, KV head, row
-// tile) items are laid end to end in units of positions, and every block takes
-// an equal run of units. Items that end up in several blocks leave their
-// parts (float32, not normalised, with m and the sum) in the workspace, and a
-// second kernel joins those.
+// The work is dealt by its amount, whatever the lengths: all (request, KV head,
+// row tile) items are laid end to end in units of positions, and the blocks take
+// runs of ceil(units / blocks) of them in turn, as far as they go: the last ones
+// may have none, and a call of few units runs on the first XCDs alone. Items that
+// end up in several blocks leave their parts (float32, not normalised, with m and
+// the sum) in the workspace, and a second kernel joins those.
 #include "tg_kv.h"
 #include "tg_tree.h"
 
@@ -185,7 +187,7 @@ struct Piece {
   bool whole;
 };
 
-// Deals the units to the blocks in equal runs; the units before each request
+// Deals the units to the blocks in runs of one length; the units before each request
 // are kept in LDS. Up to 64 requests are summed in the lanes of each wave, so
 // that the first piece needs one round of loads.
 template <int kRows, int kUnit>

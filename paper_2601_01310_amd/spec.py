@@ -6,7 +6,10 @@ Objects bind their tensors once, as :class:`tg.EwForward` does, so that a
 decode loop's calls allocate nothing: new values go into the bound tensors in
 place. A call runs on the tensors' device, whichever is current, on ``stream``
 or on that device's current stream; who passes another stream than the tensors'
-own orders it behind what filled them and keeps them until it is done. ::
+own orders it behind what filled them and keeps them until it is done. An object
+has one workspace, one set of outputs and one argument block, so its calls follow
+one another: one thread and one stream at a time (others behind an event), and an
+object of its own for each that runs beside it. ::
 
     cache = KvCache.empty(n_layers=32, n_pages=4096, page_size=16, Hkv=8, D=128,
                           B=64, max_pages=64, device="cuda")
