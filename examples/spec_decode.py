@@ -109,7 +109,7 @@ class Worker:
     def prefill(self, prompts):
         """All but the last token of each prompt into the cache, in chains."""
         todo = [list(p[:-1]) for p in prompts]
-        most = self.T // self.B
+        most = min(self.T // self.B, 63)  # a row's mask is one signed word here
         while any(todo):
             part = [t[:most] for t in todo]
             todo = [t[most:] for t in todo]
