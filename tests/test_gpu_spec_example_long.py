@@ -20,6 +20,13 @@ def test_long_answers_have_their_pages(ex):  # noqa: F811
     assert worker.cache.held.tolist() == held and int(worker.cache.refcount.sum()) == sum(held)
 
 
+def test_longer_answers_are_the_greedy_ones_up_to_ties(ex):  # noqa: F811
+    print("[gpu] speculative decoding, 250 tokens of 4 requests", flush=True)
+    tokens, one_by_one, steps = ex.main(250)  # raises where they part without a tie
+    assert [len(t) for t in tokens] == [len(t) for t in one_by_one] == [250] * 4
+    assert steps < 200
+
+
 def test_prompts_in_chunks_of_any_size_give_the_same_cache(ex):  # noqa: F811
     print("[gpu] a prompt of 150 tokens in chunks of 1, 32 and 63 rows", flush=True)
     w, prompt = ex.weights("cuda"), [(7 * i * i) % ex.VOCAB for i in range(150)]
