@@ -377,6 +377,8 @@ tg_status tg_kv_restore(const void* store, size_t store_bytes, const uint64_t* c
  * j / 64). NULL means a chain: node i sees nodes 0 .. i. lengths [B] are the
  * tokens already in the cache; node j's keys and values lie at position
  * lengths[b] + j.
+ *
+ * Argument structs start from zeros: a field that is not set is absent.
  */
 #define TG_MAX_NODES 1024
 
