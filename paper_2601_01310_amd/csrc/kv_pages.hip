@@ -131,11 +131,13 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
   __shared__ int any_copies;
   const FirstRefs ahead(refs, n_pages);
   const int page = 1 << page_shift;
-  // The shared pages among those of request b's new rows. Until the rows' own
-  // slots are written, slots[first[b] + i] keeps the page that replaces the
-  // i-th, then the page that it replaced.
-  auto shared_of = [&](int b, int n, int L, int has, auto f) {
-    return shared_pages(table + (long)b * max_pages, refs, n_pages, page_shift, L, n, has, f);
+  // The shared pages among those of request b's new rows (of the n from row `at`
+  // on, those that have slots). Until the rows' own slots are written,
+  // slots[first[b] + i] keeps the page that replaces the i-th, then the page
+  // that it replaced.
+  auto shared_of = [&](int b, int at, int n, int L, int has, auto f) {
+    const int rows = at >= 0 && at < T ? min(n, T - at) : 0;
+    return shared_pages(table + (long)b * max_pages, refs, n_pages, page_shift, L, rows, has, f);
   };
   if (threadIdx.x == 0) any_copies = 0;
   int want = 0;
@@ -151,7 +153,7 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
       len[b] = pages <= max_pages ? L : -1;
       copies[b] = 0;
       if (pages <= max_pages) {
-        if (at >= 0 && n <= T - at) copies[b] = shared_of(b, n, L, has, [](int, int, int) {});
+        copies[b] = shared_of(b, at, n, L, has, [](int, int, int) {});
         need = max(0, (int)pages - has) + copies[b];
       }
     }
@@ -192,7 +194,7 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
     const int lane = threadIdx.x % kWave;
     for (int b = 0; b < B; ++b) {
       if (copies[b] == 0) continue;
-      shared_of(b, first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
+      shared_of(b, first[b], first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
         const int rows = j == len[b] >> page_shift ? len[b] & (page - 1) : 0;
         const int fresh = slots[first[b] + i], chunks = rows * (width / 8);
         for (int l = threadIdx.x / kWave; l < 2 * n_layers; l += kWaves) {
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(kBlock) void reserve_kernel(
     __syncthreads();
     for (int b = threadIdx.x; b < B; b += kBlock)
       if (copies[b])
-        shared_of(b, first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
+        shared_of(b, first[b], first[b + 1] - first[b], len[b], held[b], [&](int i, int j, int p) {
           table[(long)b * max_pages + j] = slots[first[b] + i];
           slots[first[b] + i] = p;
         });

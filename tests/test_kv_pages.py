@@ -154,3 +154,23 @@ def test_rows_of_no_request_get_no_slots(lib):
         lib.reserve(_p(table), _p(held), _p(refs), 4, 4, B, 2, _p(held), _p(off), T, _p(slots),
                     _p(status), _p(rows), _p(rows), 1, 64)
         assert (slots == -1).all() and (refs == 0).all()
+
+
+@pytest.mark.parametrize("T", [0, 1, 3, 9])
+def test_rows_past_the_slots_change_nothing_about_sharing(lib, T):
+    """Fewer slots than rows: those that there are lie in pages of one holder."""
+    c = Cache(lib, 2, 8, 4, 5)
+    c.reserve([0, 0], [12, 0])
+    c.oracle.fork(np.array([12, 0], np.int32), [0], [1])
+    c.sync()
+    before = c.tokens(0, 12), c.tokens(1, 2)
+    lengths, off = np.array([12, 2], np.int32), np.array([0, 0, 10], np.int32)
+    slots, status = np.full(max(T, 1), 77, np.int32), np.zeros(2, np.int32)
+    lib.reserve(_p(c.table), _p(c.held), _p(c.ref), 8, 2, 2, 5, _p(lengths), _p(off), T, _p(slots),
+                _p(status), *map(_p, c.rows), 2, c.row)
+    assert status.tolist() == [1, 1] and (slots[T:] == 77).all()
+    assert all(c.ref[p] == 1 for p in slots[:T] // 4)
+    for x in c.rows:
+        x[:, slots[:T] // 4, slots[:T] % 4] = 1
+    c.oracle.table, c.oracle.caches = c.table, c.rows
+    assert np.array_equal(c.tokens(0, 12), before[0]) and np.array_equal(c.tokens(1, 2), before[1])
