@@ -228,6 +228,45 @@ tg_status tg_ew_forward_timed(const tg_ew_args* a, void* ws, size_t ws_bytes, vo
 tg_status tg_ew_forward_noalloc(const tg_ew_args* a, void* stream);
 
 /*
+ * The EW forward for a few tokens (a decode step of few requests), in two
+ * kernels that stream the touched slots' weights (three with w_gate): gating, the
+ * routing table, the SwiGLU experts and the weighted sum of tg_ew_forward, for
+ * T <= TG_MAX_FEW tokens with T * k <= TG_MAX_FEW_PAIRS.
+ *
+ * ids, weights, slots and n_unserved have tg_ew_forward's bits. The experts'
+ * outputs are summed in float32 without being rounded for each pair,
+ *   h[t,j] = bf16(silu(x W1^T) * (x W3^T)),
+ *   out[t] = bf16(sum_j topk_w[t,j] * (h[t,j] W2^T))   in rank order,
+ * so out differs from tg_ew_forward's in its last bits. A token's result depends
+ * neither on the other tokens of the batch nor on which slot of its experts,
+ * with the same weights, serves it.
+ *
+ * weights TG_WEIGHTS_BF16: ew.w13 and ew.w2 as in tg_ew_args, scales NULL.
+ * TG_WEIGHTS_F8: they point to 8-bit values (e4m3: 4 exponent and 3 mantissa
+ * bits, largest 448, no infinities) in the same layout, and the weight is value *
+ * scale with one float32 scale for each block of 128 x 128: w13_scale
+ * [S, 2I/128, d/128] and w2_scale [S, d/128, I/128]; d and I are multiples of
+ * 128. Products are bf16 x bf16 (8-bit values are exact in bf16) with float32
+ * sums, multiplied by the scale every 128 products.
+ *
+ * ew.slot_counts, slot_offsets, pair_row and y must be NULL: nothing is permuted,
+ * and a few tokens are forwarded again rather than replayed.
+ */
+#define TG_MAX_FEW 32
+#define TG_MAX_FEW_PAIRS 256
+#define TG_WEIGHTS_BF16 0
+#define TG_WEIGHTS_F8 1
+typedef struct {
+  tg_ew_args ew;
+  int weights;            /* TG_WEIGHTS_BF16 or TG_WEIGHTS_F8 */
+  const float* w13_scale; /* [S, 2I/128, d/128], or NULL */
+  const float* w2_scale;  /* [S, d/128, I/128], or NULL */
+} tg_ew_few_args;
+
+size_t tg_ew_few_workspace(const tg_ew_few_args* a);
+tg_status tg_ew_few(const tg_ew_few_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Replay of failed pairs (§5.1): after a forward, slots may fail (or be
  * restored) before its result is used. Experts are stateless and
  * deterministic, so a pair whose slot has failed is recomputed on the next

@@ -24,8 +24,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}"]
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-munsafe-fp-atomics"]
 
-SOURCES = ["gate_topk.hip", "dispatch.hip", "grouped_gemm.hip", "combine.hip", "trigger.hip",
-           "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip", "tree_attention.hip",
+SOURCES = ["gate_topk.hip", "dispatch.hip", "grouped_gemm.hip", "combine.hip", "ew_few.hip",
+           "trigger.hip", "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip", "tree_attention.hip",
            "verify_tree.hip", "kv_pages.hip", "kv_api.cpp", "tg_api.cpp"]
 
 

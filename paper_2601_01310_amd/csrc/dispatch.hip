@@ -26,6 +26,7 @@
 // copy is fully coalesced without staging).
 #include "tg_device.h"
 #include "tg_launch.h"
+#include "tg_route.h"
 #include "tg_shapes.h"
 
 namespace tg {
@@ -35,32 +36,6 @@ constexpr int kMaxS = 1024;
 constexpr int kBlock = 256;
 constexpr int kSmallHist = 1024;  // entries that a scatter block loads as they lie,
 constexpr int kSmallChunks = 32;  // of at most so many chunks
-
-// Slot of a pair of expert e: the first live ERT candidate of e.
-// REPLAY: -1 also when the first pass's slot pr is still alive (its result
-// stands). *unserved: the expert lists a local candidate, none alive.
-template <bool REPLAY>
-__device__ __forceinline__ int resolve_expert(int e, int pr, const int32_t* __restrict__ ert,
-                                              int E, int R, const uint8_t* __restrict__ alive,
-                                              int S, bool* unserved) {
-  int slot = -1;
-  bool listed = false;
-  if (e >= 0 && e < E) {
-    for (int r = 0; r < R; ++r) {
-      const int c = ert[(size_t)e * R + r];
-      if (c >= 0 && c < S) {
-        listed = true;
-        if (alive[c]) {
-          slot = c;
-          break;
-        }
-      }
-    }
-  }
-  *unserved = slot < 0 && listed;
-  if (REPLAY && pr >= 0 && pr < S && alive[pr]) slot = -1;  // first-pass result stands
-  return slot;
-}
 
 // Slot that pair p is computed on: the first live ERT candidate of its
 // expert; -2 for a token outside the batch. REPLAY: -1 also when the first

@@ -190,6 +190,38 @@ tg_status check_ew(const tg_ew_args* a) {
   return TG_OK;
 }
 
+tg_status check_few(const tg_ew_few_args* a) {
+  if (!a) return fail(TG_ERR_NULL_ARG, "args is NULL");
+  tg_ew_args any = a->ew;
+  if (any.T == 0) {  // arrays without elements may be NULL
+    if (!any.x) any.x = any.w13;
+    if (!any.out) any.out = const_cast<uint16_t*>(any.w13);
+    if (!any.w_gate && !any.logits_in) any.w_gate = any.w13;
+  }
+  const tg_status st = check_ew(&any);
+  if (st != TG_OK) return st;
+  const tg_ew_args* e = &a->ew;
+  if (e->T > TG_MAX_FEW || e->T * e->k > TG_MAX_FEW_PAIRS)
+    return fail(TG_ERR_UNSUPPORTED, "T=%d exceeds %d, or T * k=%d %d: use tg_ew_forward", e->T,
+                TG_MAX_FEW, e->T * e->k, TG_MAX_FEW_PAIRS);
+  if (e->slot_counts || e->slot_offsets || e->pair_row || e->y)
+    return fail(TG_ERR_UNSUPPORTED, "slot_counts, slot_offsets, pair_row and y must be NULL");
+  if (a->weights != TG_WEIGHTS_BF16 && a->weights != TG_WEIGHTS_F8)
+    return fail(TG_ERR_BAD_DIM, "weights=%d is neither TG_WEIGHTS_BF16 nor TG_WEIGHTS_F8",
+                a->weights);
+  const bool f8 = a->weights == TG_WEIGHTS_F8;
+  if (f8 != (a->w13_scale != nullptr) || f8 != (a->w2_scale != nullptr))
+    return fail(TG_ERR_NULL_ARG, "8-bit weights have w13_scale and w2_scale, bf16 weights none");
+  if (f8 && (e->d % 128 || e->I % 128))
+    return fail(TG_ERR_UNSUPPORTED, "d=%d and I=%d must be multiples of 128 for 8-bit weights",
+                e->d, e->I);
+  const void* const loaded[] = {e->x, e->w_gate, e->w13, e->w2};
+  for (const void* p : loaded)
+    if (reinterpret_cast<uintptr_t>(p) & 15)
+      return fail(TG_ERR_UNSUPPORTED, "x and the weights must be 16-byte aligned");
+  return TG_OK;
+}
+
 }  // namespace
 
 namespace tg {
@@ -377,6 +409,21 @@ size_t tg_ew_forward_workspace(const tg_ew_args* a) {
 
 tg_status tg_ew_forward(const tg_ew_args* a, void* ws, size_t ws_bytes, void* stream) {
   return tg::ew_forward(a, ws, ws_bytes, stream, nullptr);
+}
+
+size_t tg_ew_few_workspace(const tg_ew_few_args* a) {
+  return check_few(a) == TG_OK ? tg::ew_few_workspace_bytes(a) : 0;
+}
+
+tg_status tg_ew_few(const tg_ew_few_args* a, void* ws, size_t ws_bytes, void* stream) {
+  const tg_status st = check_few(a);
+  if (st != TG_OK) return st;
+  const size_t need = tg::ew_few_workspace_bytes(a);
+  if (!ws || ws_bytes < need)
+    return fail(TG_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws_bytes);
+  if (reinterpret_cast<uintptr_t>(ws) & 255)
+    return fail(TG_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  return hip_status(tg::launch_ew_few(a, ws, static_cast<hipStream_t>(stream)), "tg_ew_few");
 }
 
 tg_status tg_ew_forward_timed(const tg_ew_args* a, void* ws, size_t ws_bytes, void* stream,

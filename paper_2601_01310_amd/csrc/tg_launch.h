@@ -109,6 +109,10 @@ hipError_t launch_recombine(const uint16_t* y, const int32_t* pair_row, const in
                             const int32_t* replay_row, const float* w, int T, int k, int d,
                             uint16_t* out, hipStream_t stream);
 
+// The forward of a few tokens (checked by the caller).
+size_t ew_few_workspace_bytes(const tg_ew_few_args* a);
+hipError_t launch_ew_few(const tg_ew_few_args* a, void* ws, hipStream_t stream);
+
 // Partial-batch trigger (one block): waits until every live AW has
 // delivered, or the delivered rows of live AWs reach min_rows, or spin_limit
 // polls have passed; then marks the rows of the delivered live AWs in

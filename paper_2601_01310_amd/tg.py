@@ -22,6 +22,7 @@ EXPORTS = [
     "tg_status_string", "tg_last_error", "tg_gate_topk", "tg_remap_dispatch_workspace",
     "tg_remap_dispatch", "tg_expert_ffn_grouped", "tg_set_gemm_tile_policy", "tg_combine",
     "tg_ew_forward_workspace", "tg_ew_forward", "tg_ew_forward_timed", "tg_ew_forward_noalloc",
+    "tg_ew_few_workspace", "tg_ew_few",
     "tg_ew_replay_workspace", "tg_ew_replay", "tg_batch_trigger", "tg_kv_checkpoint",
     "tg_kv_checkpoint_strided", "tg_kv_restore", "tg_qk_norm_rope", "tg_tree_attention_workspace",
     "tg_tree_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_kv_compact",
@@ -46,6 +47,12 @@ class EwArgs(ctypes.Structure):
             "topk_w", "pair_slot", "slot_counts", "slot_offsets", "pair_row", "n_unserved", "y",
             "token_valid")
     ]
+
+
+class EwFewArgs(ctypes.Structure):
+    """Mirror of ``tg_ew_few_args``."""
+    _fields_ = [("ew", EwArgs), ("weights", ctypes.c_int), ("w13_scale", ctypes.c_void_p),
+                ("w2_scale", ctypes.c_void_p)]
 
 
 class ReplayArgs(ctypes.Structure):
@@ -134,6 +141,10 @@ def load(path: Optional[str] = None):
                                         ctypes.POINTER(ctypes.c_void_p), i]
     lib.tg_ew_forward_noalloc.restype = i
     lib.tg_ew_forward_noalloc.argtypes = [ctypes.POINTER(EwArgs), vp]
+    lib.tg_ew_few_workspace.restype = sz
+    lib.tg_ew_few_workspace.argtypes = [ctypes.POINTER(EwFewArgs)]
+    lib.tg_ew_few.restype = i
+    lib.tg_ew_few.argtypes = [ctypes.POINTER(EwFewArgs), vp, sz, vp]
     lib.tg_ew_replay_workspace.restype = sz
     lib.tg_ew_replay_workspace.argtypes = [ctypes.POINTER(ReplayArgs)]
     lib.tg_ew_replay.restype = i
@@ -431,3 +442,68 @@ class EwForward:
         r["args"].slot_alive = _p(alive)
         tg_ew_replay(r["args"], r["ws"], r["ws_bytes"], stream)
         return r["replay_slot"], r["n_replayed"], r["n_unserved"]
+
+
+MAX_FEW = 32  # TG_MAX_FEW in tg.h
+WEIGHTS_BF16, WEIGHTS_F8 = 0, 1
+
+
+class EwFew:
+    """The EW forward for a few tokens, ``x`` [T, d] bf16 with T <= MAX_FEW: two
+    kernels that stream the touched slots' weights. ``w_gate`` [E, d] bf16 or
+    ``logits`` [T, E] float32; ``ert`` [E, R] int32 and ``alive`` [S] uint8 as
+    :class:`EwForward` has them; ``w13`` [S, 2I, d] and ``w2`` [S, d, I] bf16, or
+    float8_e4m3fn with ``w13_scale`` [S, 2I/128, d/128] and ``w2_scale`` [S, d/128,
+    I/128] float32. ``token_valid`` [T] uint8 leaves tokens out.
+
+    The tensors are bound once, so that a decode loop's calls allocate nothing;
+    the object has one workspace and one set of outputs (``out``, ``topk_ids``,
+    ``topk_w``, ``pair_slot``, ``n_unserved``), so its calls follow one another: one
+    stream at a time, and an object of its own for each that runs beside it."""
+
+    def __init__(self, x, w_gate, logits, ert, alive, w13, w2, k, w13_scale=None, w2_scale=None,
+                 token_valid=None):
+        from . import spec  # which builds on this module
+        T, d = x.shape
+        (E, R), (S, I2, _) = ert.shape, w13.shape
+        f8 = w13.dtype == torch.float8_e4m3fn
+        weights = torch.float8_e4m3fn if f8 else torch.bfloat16
+        I = I2 // 2
+        want = dict(x=(x, torch.bfloat16, (T, d)), w_gate=(w_gate, torch.bfloat16, (E, d)),
+                    logits=(logits, torch.float32, (T, E)), ert=(ert, torch.int32, (E, R)),
+                    alive=(alive, torch.uint8, (S,)), w13=(w13, weights, (S, 2 * I, d)),
+                    w2=(w2, weights, (S, d, I)),
+                    w13_scale=(w13_scale, torch.float32, (S, 2 * I // 128, d // 128)),
+                    w2_scale=(w2_scale, torch.float32, (S, d // 128, I // 128)),
+                    token_valid=(token_valid, torch.uint8, (T,)))
+        for name, (t, dtype, shape) in want.items():
+            if t is None:
+                continue
+            if t.dtype != dtype or tuple(t.shape) != shape:
+                raise ValueError(f"{name} is {list(t.shape)} {t.dtype}, {list(shape)} {dtype} required")
+            if t.device != x.device:
+                raise ValueError(f"{name} lies on {t.device}, x on {x.device}")
+        dev = x.device
+        self.out = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+        self.topk_ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+        self.topk_w = torch.empty((T, k), dtype=torch.float32, device=dev)
+        self.pair_slot = torch.empty((T, k), dtype=torch.int32, device=dev)
+        self.n_unserved = torch.empty((1,), dtype=torch.int32, device=dev)
+        self._keep = [t for t, _, _ in want.values()]
+        a = self.args = EwFewArgs()
+        a.ew = make_ew_args(T, d, E, k, I, S, R, x, w_gate, logits, ert, alive, w13, w2, self.out,
+                            self.topk_ids, self.topk_w, self.pair_slot,
+                            n_unserved=self.n_unserved, token_valid=token_valid)
+        a.weights = WEIGHTS_F8 if f8 else WEIGHTS_BF16
+        a.w13_scale, a.w2_scale = _p(w13_scale), _p(w2_scale)
+        lib = load()
+        self._ref, self._device, self._call = ctypes.byref(a), x.get_device(), lib.tg_ew_few
+        self.ws_bytes = int(lib.tg_ew_few_workspace(self._ref))
+        if self.ws_bytes == 0:
+            raise TgError(lib.tg_ew_few(self._ref, None, 0, None), "workspace")
+        self.ws = workspace(self.ws_bytes, dev)
+        self._ws, self._run = self.ws.data_ptr(), spec._run
+
+    def __call__(self, stream=None):
+        self._run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
+        return self.out
