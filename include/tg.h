@@ -423,6 +423,7 @@ tg_status tg_kv_restore(const void* store, size_t store_bytes, const uint64_t* c
 
 #define TG_BF16 0
 #define TG_F16 1
+#define TG_F32 2 /* logits only */
 
 /*
  * A paged KV cache. Position p of request b lies in row p % page_size of
@@ -570,6 +571,48 @@ typedef struct {
 
 size_t tg_verify_tree_workspace(const tg_verify_args* a);
 tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The next token of every row from its logits, and the distribution that it was
+ * drawn from (the target_probs of tg_verify_tree).
+ *
+ * Row t of logits [T, V] (logits_stride elements from row to row) gives token i
+ * the weight w_i = e^((l_i - l_max) / temperature[t]). The likelier token has the
+ * larger logit, of equal ones the lower index. What stays, in this order:
+ *   top_k[t] > 0    the top_k[t] likeliest tokens;
+ *   top_p[t] < 1    of those, each whose likelier ones have less than top_p[t] of
+ *                   their mass together (the likeliest always);
+ *   min_p[t] > 0    of those, each with w_i >= min(min_p[t], 1).
+ * Drawn: the lowest token whose cumulative mass, in token order, exceeds u[t]
+ * (clamped into [0, 1), NaN = 0) times the mass of all that stay. temperature[t]
+ * <= 0 or NaN: the likeliest token, whatever u and the filters are. Arrays that are
+ * NULL stand for temperature 1 and no filter; a NaN filter is none.
+ *
+ * Weights are exact to 2^-42 of themselves and counted in units of at most
+ * 2^(1 - s), s = min(45, 62 - ceil(log2 V)); what is less counts for nothing. Their
+ * sums and shares of them are exact, and a row's result does not depend on the
+ * other rows. Logits of -infinity or NaN are no tokens, +infinity counts as the
+ * largest float32. A row without tokens gives -1. probs [T, V] float32 (NULL: not
+ * wanted; rows probs_stride apart) gets w_i over the mass of all that stay, 0 for
+ * the others, and 0 everywhere for a row without tokens. Limits: V <= 2^24,
+ * T * ceil(V / 8192) < 2^31; logits aligned to their type.
+ */
+typedef struct {
+  int dtype; /* of logits: TG_F32, TG_BF16 or TG_F16 */
+  int T, V;
+  int64_t logits_stride, probs_stride; /* elements from row to row */
+  const void* logits;
+  const float* u;           /* [T] */
+  const float* temperature; /* [T] or NULL */
+  const int32_t* top_k;     /* [T] or NULL */
+  const float* top_p;       /* [T] or NULL */
+  const float* min_p;       /* [T] or NULL */
+  int32_t* tokens;          /* [T] */
+  float* probs;             /* [T, V] or NULL */
+} tg_sample_args;
+
+size_t tg_sample_workspace(const tg_sample_args* a);
+tg_status tg_sample(const tg_sample_args* a, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * The rows kept by tg_verify_tree moved together: in every layer, K and V of

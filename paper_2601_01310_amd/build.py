@@ -26,7 +26,8 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
 
 SOURCES = ["gate_topk.hip", "dispatch.hip", "grouped_gemm.hip", "combine.hip", "ew_few.hip",
            "trigger.hip", "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip", "tree_attention.hip",
-           "verify_tree.hip", "kv_pages.hip", "kv_api.cpp", "tg_api.cpp"]
+           "verify_tree.hip", "sample.hip", "kv_pages.hip",
+           "kv_api.cpp", "tg_api.cpp"]
 
 
 def _compile(src: str) -> str:

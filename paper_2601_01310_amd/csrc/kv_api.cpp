@@ -158,6 +158,24 @@ tg_status check_verify(const tg_verify_args* a) {
   return TG_OK;
 }
 
+tg_status check_sample(const tg_sample_args* a) {
+  if (!a) return set_error(TG_ERR_NULL_ARG, "args is NULL");
+  if (a->dtype != TG_F32 && a->dtype != TG_BF16 && a->dtype != TG_F16)
+    return set_error(TG_ERR_BAD_DIM, "dtype=%d is neither TG_F32, TG_BF16 nor TG_F16", a->dtype);
+  if (a->T < 0 || a->V <= 0)
+    return set_error(TG_ERR_BAD_DIM, "T=%d must be >= 0 and V=%d > 0", a->T, a->V);
+  if (a->V > (1 << 24)) return set_error(TG_ERR_UNSUPPORTED, "V=%d exceeds 2^24", a->V);
+  if ((long long)a->T * ((a->V + 8191) / 8192) >= (1LL << 31))  // blocks are counted in 32 bits
+    return set_error(TG_ERR_UNSUPPORTED, "T=%d rows of %d logits are too many", a->T, a->V);
+  if (a->logits_stride < a->V || (a->probs && a->probs_stride < a->V))
+    return set_error(TG_ERR_BAD_DIM, "a row of logits or probabilities is longer than its stride");
+  if (a->T > 0 && (!a->logits || !a->u || !a->tokens))
+    return set_error(TG_ERR_NULL_ARG, "a required pointer is NULL");
+  if (!aligned(a->logits, a->dtype == TG_F32 ? 4 : 2) || !aligned(a->probs, 4))
+    return set_error(TG_ERR_UNSUPPORTED, "logits and probs must be aligned to their type");
+  return TG_OK;
+}
+
 tg_status check_workspace(const void* ws, size_t given, size_t need) {
   if (!ws || given < need)
     return set_error(TG_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, given);
@@ -196,6 +214,17 @@ tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, voi
   if (st != TG_OK) return st;
   if ((st = check_workspace(ws, ws_bytes, tg::verify_workspace_bytes(a))) != TG_OK) return st;
   return done(tg::launch_verify_tree(a, ws, static_cast<hipStream_t>(stream)), "tg_verify_tree");
+}
+
+size_t tg_sample_workspace(const tg_sample_args* a) {
+  return check_sample(a) == TG_OK ? tg::sample_workspace_bytes(a) : 0;
+}
+
+tg_status tg_sample(const tg_sample_args* a, void* ws, size_t ws_bytes, void* stream) {
+  tg_status st = check_sample(a);
+  if (st != TG_OK) return st;
+  if ((st = check_workspace(ws, ws_bytes, tg::sample_workspace_bytes(a))) != TG_OK) return st;
+  return done(tg::launch_sample(a, ws, static_cast<hipStream_t>(stream)), "tg_sample");
 }
 
 tg_status tg_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,

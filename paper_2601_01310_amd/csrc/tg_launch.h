@@ -146,6 +146,8 @@ size_t tree_attention_workspace_bytes(const tg_tree_attn_args* a);
 hipError_t launch_tree_attention(const tg_tree_attn_args* a, void* ws, hipStream_t stream);
 size_t verify_workspace_bytes(const tg_verify_args* a);
 hipError_t launch_verify_tree(const tg_verify_args* a, void* ws, hipStream_t stream);
+size_t sample_workspace_bytes(const tg_sample_args* a);
+hipError_t launch_sample(const tg_sample_args* a, void* ws, hipStream_t stream);
 hipError_t launch_kv_compact(const tg_kv_cache* c, const int32_t* path, int max_path,
                              const int32_t* n_keep, const int32_t* lengths, int32_t* new_lengths,
                              hipStream_t stream);

@@ -28,6 +28,7 @@ import torch
 from . import tg
 
 _DTYPES = {torch.bfloat16: tg.BF16, torch.float16: tg.F16}
+_LOGITS = {torch.float32: tg.F32, **_DTYPES}
 
 
 def _want(t: Optional[torch.Tensor], name: str, dtype, shape=None, optional=False):
@@ -325,3 +326,52 @@ class VerifyTree:
     def __call__(self, stream=None):
         _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
         return self.tokens_out, self.path, self.n_out
+
+
+class SampleTokens:
+    """The next tokens of ``logits`` [T, V] (float32, bfloat16 or float16, dense
+    rows) by the random numbers ``u`` [T] float32 in [0, 1). ``temperature`` [T]
+    float32 (0: the likeliest token), ``top_k`` [T] int32 (0: all), ``top_p`` [T]
+    float32 (1: all) and ``min_p`` [T] float32 (0: all), or None. Returns tokens [T]
+    int32 (-1 for a row without tokens), and with ``probs`` (True, or a [T, V]
+    float32 tensor) the distributions that they were drawn from."""
+
+    def __init__(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, probs=False):
+        if logits.dim() != 2:
+            raise ValueError(f"logits is {list(logits.shape)}, [T, V] required")
+        T, V = logits.shape
+        if logits.dtype not in _LOGITS:
+            raise ValueError(f"logits is {logits.dtype}, float32, bfloat16 or float16 required")
+        stride = max(V, _rows(logits, "logits", logits.dtype, (V,)))
+        _want(u, "u", torch.float32, (T,))
+        _want(temperature, "temperature", torch.float32, (T,), optional=True)
+        _want(top_k, "top_k", torch.int32, (T,), optional=True)
+        _want(top_p, "top_p", torch.float32, (T,), optional=True)
+        _want(min_p, "min_p", torch.float32, (T,), optional=True)
+        if probs is True:
+            probs = torch.empty((T, V), dtype=torch.float32, device=logits.device)
+        self.probs = None if probs is False else probs
+        probs_stride = V
+        if self.probs is not None:
+            probs_stride = max(V, _rows(self.probs, "probs", torch.float32, (V,)))
+            if self.probs.shape[0] != T:
+                raise ValueError(f"probs has {self.probs.shape[0]} rows, {T} required")
+        _same_device(logits, u, temperature, top_k, top_p, min_p, self.probs)
+        self.tokens = torch.empty((T,), dtype=torch.int32, device=logits.device)
+        self._keep = (logits, u, temperature, top_k, top_p, min_p)
+        a = self.args = tg.SampleArgs()
+        a.dtype, a.T, a.V = _LOGITS[logits.dtype], T, V
+        a.logits_stride, a.probs_stride = stride, probs_stride
+        for name, t in dict(logits=logits, u=u, temperature=temperature, top_k=top_k, top_p=top_p,
+                            min_p=min_p, tokens=self.tokens, probs=self.probs).items():
+            setattr(a, name, None if t is None else t.data_ptr())
+        self.ws_bytes = tg.tg_sample_workspace(a)
+        if self.ws_bytes == 0:
+            raise tg.TgError(tg.load().tg_sample(ctypes.byref(a), None, 0, None), "workspace")
+        self.ws = tg.workspace(self.ws_bytes, logits.device)
+        self._ref, self._device = ctypes.byref(a), logits.get_device()
+        self._ws, self._call = self.ws.data_ptr(), tg.load().tg_sample
+
+    def __call__(self, stream=None):
+        _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
+        return self.tokens if self.probs is None else (self.tokens, self.probs)

@@ -25,7 +25,8 @@ EXPORTS = [
     "tg_ew_few_workspace", "tg_ew_few",
     "tg_ew_replay_workspace", "tg_ew_replay", "tg_batch_trigger", "tg_kv_checkpoint",
     "tg_kv_checkpoint_strided", "tg_kv_restore", "tg_qk_norm_rope", "tg_tree_attention_workspace",
-    "tg_tree_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_kv_compact",
+    "tg_tree_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_sample_workspace",
+    "tg_sample", "tg_kv_compact",
     "tg_kv_pages_reserve", "tg_kv_pages_fork", "tg_kv_pages_trim",
 ]
 
@@ -101,7 +102,14 @@ class VerifyArgs(ctypes.Structure):
                 "path n_out status")])
 
 
-BF16, F16 = 0, 1
+class SampleArgs(ctypes.Structure):
+    """Mirror of ``tg_sample_args``."""
+    _fields_ = _fields([
+        ("int", "dtype T V"), ("i64", "logits_stride probs_stride"),
+        ("ptr", "logits u temperature top_k top_p min_p tokens probs")])
+
+
+BF16, F16, F32 = 0, 1, 2
 MAX_NODES = 1024  # TG_MAX_NODES in tg.h
 
 
@@ -162,7 +170,8 @@ def load(path: Optional[str] = None):
     kv = ctypes.POINTER(KvCacheArgs)
     lib.tg_qk_norm_rope.restype = i
     lib.tg_qk_norm_rope.argtypes = [ctypes.POINTER(QkArgs), vp]
-    for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_verify_tree", VerifyArgs)):
+    for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_verify_tree", VerifyArgs),
+                       ("tg_sample", SampleArgs)):
         size, call = getattr(lib, name + "_workspace"), getattr(lib, name)
         size.restype, size.argtypes = sz, [ctypes.POINTER(args)]
         call.restype, call.argtypes = i, [ctypes.POINTER(args), vp, sz, vp]
@@ -346,6 +355,10 @@ def tg_tree_attention_workspace(args: TreeAttnArgs) -> int:
 
 def tg_verify_tree_workspace(args: VerifyArgs) -> int:
     return int(load().tg_verify_tree_workspace(ctypes.byref(args)))
+
+
+def tg_sample_workspace(args: SampleArgs) -> int:
+    return int(load().tg_sample_workspace(ctypes.byref(args)))
 
 
 def _flag_ptr(t):
