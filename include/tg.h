@@ -524,6 +524,33 @@ size_t tg_tree_attention_workspace(const tg_tree_attn_args* a);
 tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * tg_tree_attention for a batch whose groups of requests share the pages of a
+ * prefix (samples of one prompt, requests behind one system prompt or document;
+ * see tg_kv_pages_fork): each group's shared positions are read once for all its
+ * rows instead of once per request.
+ *
+ * Group g is requests group_offsets[g] .. group_offsets[g+1]-1 (device array
+ * [n_groups+1], non-decreasing, from 0 to B). The first shared[g] positions of all
+ * of them lie in the same pages: they are read through the table row of the
+ * group's first request. shared[g] may be anything from 0 on; what counts is the
+ * largest multiple of 128 that neither it nor the length of any request of the
+ * group with rows exceeds (0 for one request alone), and requests outside all
+ * groups share nothing. Results are tg_tree_attention's up to the last bits.
+ * Groups are dealt out by the mean rows of a group, T / n_groups; any are right.
+ * The limit is, besides tg_tree_attention's,
+ *   Hkv * (T * G' + n_groups) * max_pages * page_size / 64 < 2^30.
+ */
+typedef struct {
+  tg_tree_attn_args attn;
+  int n_groups;                 /* 0 .. 4096 */
+  const int32_t* group_offsets; /* [n_groups+1] */
+  const int32_t* shared;        /* [n_groups] */
+} tg_prefix_attn_args;
+
+size_t tg_prefix_attention_workspace(const tg_prefix_attn_args* a);
+tg_status tg_prefix_attention(const tg_prefix_attn_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Which drafted tokens stay, and the token that follows them.
  *
  * target_probs [T, V] float32 (rows target_stride apart) is the target's

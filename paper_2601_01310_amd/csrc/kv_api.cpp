@@ -141,6 +141,26 @@ tg_status check_attn(const tg_tree_attn_args* a) {
   return TG_OK;
 }
 
+tg_status check_prefix(const tg_prefix_attn_args* a) {
+  if (!a) return set_error(TG_ERR_NULL_ARG, "args is NULL");
+  const tg_tree_attn_args* x = &a->attn;
+  const tg_status st = check_attn(x);
+  if (st != TG_OK) return st;
+  if (a->n_groups < 0) return set_error(TG_ERR_BAD_DIM, "n_groups=%d must be >= 0", a->n_groups);
+  if (a->n_groups > 4096)
+    return set_error(TG_ERR_UNSUPPORTED, "n_groups=%d exceeds 4096", a->n_groups);
+  if (a->n_groups > 0 && (!a->group_offsets || !a->shared))
+    return set_error(TG_ERR_NULL_ARG, "group_offsets and shared are required");
+  // Units of the groups' work, as in check_attn.
+  const long long G = x->Hq / x->cache.Hkv;
+  const long long items = x->cache.Hkv * (x->T * G / 16 + a->n_groups);
+  const long long units = ((long long)x->cache.max_pages * x->cache.page_size + 63) / 64;
+  if (items > (1LL << 30) / units - 1)
+    return set_error(TG_ERR_UNSUPPORTED,
+                     "Hkv * (16-row tiles of all groups) * (positions per request) / 64 >= 2^30");
+  return TG_OK;
+}
+
 tg_status check_verify(const tg_verify_args* a) {
   if (!a) return set_error(TG_ERR_NULL_ARG, "args is NULL");
   if (a->B < 0 || a->T < 0 || a->V <= 0 || a->max_path <= 0)
@@ -203,6 +223,20 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
   if ((st = check_workspace(ws, ws_bytes, tg::tree_attention_workspace_bytes(a))) != TG_OK) return st;
   return done(tg::launch_tree_attention(a, ws, static_cast<hipStream_t>(stream)),
               "tg_tree_attention");
+}
+
+size_t tg_prefix_attention_workspace(const tg_prefix_attn_args* a) {
+  return check_prefix(a) == TG_OK ? tg::prefix_attention_workspace_bytes(a) : 0;
+}
+
+tg_status tg_prefix_attention(const tg_prefix_attn_args* a, void* ws, size_t ws_bytes,
+                              void* stream) {
+  tg_status st = check_prefix(a);
+  if (st != TG_OK) return st;
+  if ((st = check_workspace(ws, ws_bytes, tg::prefix_attention_workspace_bytes(a))) != TG_OK)
+    return st;
+  return done(tg::launch_prefix_attention(a, ws, static_cast<hipStream_t>(stream)),
+              "tg_prefix_attention");
 }
 
 size_t tg_verify_tree_workspace(const tg_verify_args* a) {

@@ -1,0 +1,388 @@
+// Attention of a batch whose groups of requests share the pages of a prefix.
+//
+// The rows of a group (all its requests' nodes) see the prefix alike, so they are
+// one item's rows there, and its keys and values are read once for up to 128 of
+// them instead of once per request; each request's own rows then see its other
+// positions. Both are the kernels of tg_attn.h, over a group's shared positions
+// and over each request's from there on, and leave, for every row and for every
+// run of positions that one block had, its maximum m_i, sum l_i and output o_i
+// (float32); a row's output is sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.
+//
+//   plan    one block: what each group really shares (not past any member's
+//           length, whole units of 128 positions), and the units of work before
+//           each group and request;
+//   prefix, tail;
+//   join    a wave takes a few heads of a row, its parts in one loop.
+#include "tg_attn.h"
+
+namespace tg {
+namespace {
+
+constexpr int kPlanBlock = 1024, kPlanWaves = kPlanBlock / kWave;
+constexpr int kMaxRequests = 4096;
+constexpr int kWholeUnits = 128;  // positions; a multiple of both kernels' units
+
+struct PlanParams {
+  int B, groups, T, max_nodes, cap, G, Hkv;
+  int prefix_rows, prefix_unit, tail_rows, tail_unit;  // of the two kernels
+  const int32_t *off, *lengths, *group_off, *shared;
+  int32_t *pre_prefix, *pre_tail;  // [groups + 1], [B + 1]
+  int32_t *from, *group_of;        // [B]
+  int32_t* request_of_row;         // [T], -1: none
+  Group* group;                    // [groups]
+};
+
+// pre[i + 1] = units(0) + ... + units(i), pre[0] = 0.
+template <class Units>
+__device__ __forceinline__ void sum_units(int n, int32_t* pre, int* carry, Units units) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int base = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanBlock) {
+    const int i = i0 + threadIdx.x;
+    int x = i < n ? units(i) : 0;
+    for (int m = 1; m < kWave; m *= 2) {
+      const int o = __shfl_up(x, m);
+      if (lane >= m) x = add_units(x, o);
+    }
+    __syncthreads();
+    if (lane == kWave - 1) carry[wave] = x;
+    __syncthreads();
+    int front = base;
+    for (int w = 0; w < kPlanWaves; ++w) {
+      if (w < wave) front = add_units(front, carry[w]);
+      base = add_units(base, carry[w]);
+    }
+    if (i < n) pre[i + 1] = add_units(front, x);
+  }
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+}
+
+// The last i in [0, n) with a[i] <= x, 0 if there is none.
+__device__ __forceinline__ int last_at(const int* a, int n, int x) {
+  int i = 0;
+  for (int hi = n; hi - i > 1;) {
+    const int mid = (i + hi) / 2;
+    if (a[mid] <= x) i = mid;
+    else hi = mid;
+  }
+  return i;
+}
+
+__global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
+  __shared__ int starts[kMaxRequests + 1];  // of groups, then of requests' rows
+  __shared__ int least[kMaxRequests];       // of a group: its shared positions
+  __shared__ int members[kMaxRequests];     // with rows
+  __shared__ int carry[kPlanWaves];
+  const int tid = threadIdx.x;
+  // Offsets that do not ascend from 0 to B stay inside all arrays.
+  for (int g = tid; g <= p.groups; g += kPlanBlock)
+    starts[g] = max(0, min(p.group_off[g], p.B));
+  for (int g = tid; g < p.groups; g += kPlanBlock) {
+    least[g] = max(0, min(p.shared[g], p.cap));
+    members[g] = 0;
+  }
+  __syncthreads();
+  for (int b = tid; b < p.B; b += kPlanBlock) {
+    int g = p.groups ? last_at(starts, p.groups, b) : -1;
+    if (g >= 0 && (b < starts[g] || b >= starts[g + 1])) g = -1;
+    p.group_of[b] = g;
+    int first, n;
+    request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
+    if (g >= 0 && n > 0) {
+      atomicMin(&least[g], max(0, p.lengths[b]));
+      atomicAdd(&members[g], 1);
+    }
+  }
+  __syncthreads();
+  // One request alone shares nothing.
+  for (int g = tid; g < p.groups; g += kPlanBlock) {
+    const int shared = members[g] > 1 ? least[g] / kWholeUnits * kWholeUnits : 0;
+    least[g] = shared;
+    Group x;
+    const int b0 = starts[g], b1 = max(b0, starts[g + 1]);
+    x.first = max(0, min(p.off[b0], p.T));
+    x.n = shared ? max(x.first, min(p.off[b1], p.T)) - x.first : 0;
+    x.positions = shared;
+    x.request = min(b0, p.B - 1);
+    p.group[g] = x;
+  }
+  __syncthreads();
+  for (int b = tid; b < p.B; b += kPlanBlock) {
+    const int g = p.group_of[b];
+    p.from[b] = g >= 0 ? least[g] : 0;
+  }
+  sum_units(p.groups, p.pre_prefix, carry, [&](int g) {
+    const Group x = p.group[g];
+    return (x.positions + p.prefix_unit - 1) / p.prefix_unit *
+           ((x.n * p.G + p.prefix_rows - 1) / p.prefix_rows) * p.Hkv;
+  });
+  sum_units(p.B, p.pre_tail, carry, [&](int b) {
+    int first, n;
+    request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
+    const int L = max(0, min(p.lengths[b], p.cap)), end = min(L + n, p.cap);
+    return (end - p.from[b] + p.tail_unit - 1) / p.tail_unit *
+           ((n * p.G + p.tail_rows - 1) / p.tail_rows) * p.Hkv;
+  });
+  for (int b = tid; b <= p.B; b += kPlanBlock) starts[b] = max(0, min(p.off[b], p.T));
+  __syncthreads();
+  for (int t = tid; t < p.T; t += kPlanBlock) {
+    const int b = last_at(starts, p.B, t);
+    p.request_of_row[t] = t >= starts[b] && t < min(starts[b + 1], starts[b] + p.max_nodes) ? b : -1;
+  }
+}
+
+// Where a kernel left its items.
+struct Parts {
+  const int32_t* pre;
+  const float* part;
+  const float2* part_ml;
+  const float* whole;
+  const float2* whole_ml;
+  int rows, unit, blocks;
+};
+
+struct JoinParams {
+  Parts prefix, tail;
+  const int32_t *off, *lengths, *from, *group_of, *request_of_row;
+  const Group* group;
+  uint16_t* out;
+  int64_t out_stride;
+  int T, Hkv, G, cap, max_nodes, B, groups;
+};
+
+// A running join of a row's parts, four columns to a lane.
+struct Joined {
+  f32x4 o = f32x4{0, 0, 0, 0};
+  float m = -INFINITY, sum = 0.0f;
+
+  __device__ __forceinline__ void add(f32x4 x, float2 ml) {
+    const float next = fmaxf(m, ml.x), a = grow(m, next), e = grow(ml.x, next);
+    m = next;
+    sum = sum * a + ml.y * e;
+    o = o * a + x * e;
+  }
+};
+
+// Adds the parts of a row: line `line` of head g of item group `b`, whose items are
+// `tiles` times `units` units; `row`: its place among whole items' rows.
+template <int D>
+__device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, int b, int g, int line,
+                                          int units, int tiles, int64_t row, int ch) {
+  if (units <= 0) return;
+  constexpr int kU = 8;
+  const int share = max(1, (total + s.blocks - 1) / s.blocks);
+  const int start = s.pre[b] + (g * tiles + line / s.rows) * units;
+  const int k0 = start / share, parts = (start + units - 1) / share - k0 + 1;
+  if (parts == 1) {
+    j.add(*reinterpret_cast<const f32x4*>(s.whole + row * D + ch * 4), s.whole_ml[row]);
+    return;
+  }
+  const int slot = start == k0 * share ? 0 : 1, at = line % s.rows;
+  for (int k = 0; k < parts; k += kU) {
+    f32x4 x[kU];
+    float2 ml[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = min(k + u, parts - 1);
+      const int block = min(k0 + i, s.blocks - 1);
+      const int64_t place = (2 * (int64_t)block + (i == 0 ? slot : 0)) * s.rows + at;
+      x[u] = *reinterpret_cast<const f32x4*>(s.part + place * D + ch * 4);
+      ml[u] = s.part_ml[place];
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (k + u < parts) j.add(x[u], ml[u]);
+  }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) {
+  constexpr int kLine = D / 4, kAt = kWave / kLine;  // lanes per row, rows per wave
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int t = blockIdx.x, Hq = p.Hkv * p.G, ch = lane % kLine;
+  const int b = p.request_of_row[t];
+  const int head = (blockIdx.y * kWaves + wave) * kAt + lane / kLine;
+  if (b < 0 || head >= Hq) return;
+  const int g = head / p.G, jj = head - g * p.G;
+  const int from = p.from[b];
+  int first, n;
+  request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
+  const int L = max(0, min(p.lengths[b], p.cap)), end = min(L + n, p.cap);
+  const int units = (end - from + p.tail.unit - 1) / p.tail.unit;
+  const int tiles = (n * p.G + p.tail.rows - 1) / p.tail.rows;
+  const int line = (t - first) * p.G + jj, total = p.tail.pre[p.B];
+  const int64_t row = (int64_t)t * Hq + head;
+  if (from == 0) {  // one block's rows are there already
+    const int share = max(1, (total + p.tail.blocks - 1) / p.tail.blocks);
+    const int start = p.tail.pre[b] + (g * tiles + line / p.tail.rows) * units;
+    if (start / share == (start + units - 1) / share) return;
+  }
+  Joined j;
+  add_parts<D>(j, p.tail, total, b, g, line, units, tiles, row, ch);
+  if (from > 0) {
+    const int gr = p.group_of[b];
+    const Group x = p.group[gr];
+    if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
+      add_parts<D>(j, p.prefix, p.prefix.pre[p.groups], gr, g, (t - x.first) * p.G + jj,
+                   (x.positions + p.prefix.unit - 1) / p.prefix.unit,
+                   (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch);
+  }
+  const float inv = inverse(j.sum);
+  *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + ch * 4) =
+      make_uint2(T::pack(j.o[0] * inv, j.o[1] * inv), T::pack(j.o[2] * inv, j.o[3] * inv));
+}
+
+// The kernel for the prefixes goes by the mean rows of a group.
+Shape prefix_shape(const tg_prefix_attn_args* a) {
+  const tg_tree_attn_args& x = a->attn;
+  const int groups = a->n_groups > 0 ? a->n_groups : 1;
+  return shape_for((long long)(x.T + groups - 1) / groups * (x.Hq / x.cache.Hkv), x.cache.D);
+}
+
+int blocks_of(Shape s, int D) { return kCus * occupancy(D, s.q); }
+
+struct Space {
+  int32_t *pre_prefix, *pre_tail, *from, *group_of, *request_of_row;
+  Group* group;
+  float *part[2], *whole[2];  // of the prefixes, of the tails
+  float2 *part_ml[2], *whole_ml[2];
+};
+
+Space carve(const tg_prefix_attn_args* a, char* base, size_t* bytes) {
+  size_t off = 0;
+  auto take = [&](size_t n) -> char* {
+    char* p = base ? base + off : nullptr;
+    off += (n + 255) & ~(size_t)255;
+    return p;
+  };
+  const tg_tree_attn_args& x = a->attn;
+  const size_t B = x.cache.B, G = a->n_groups, D = x.cache.D, rows = (size_t)x.T * x.Hq;
+  Space s;
+  s.pre_prefix = reinterpret_cast<int32_t*>(take((G + 1) * 4));
+  s.pre_tail = reinterpret_cast<int32_t*>(take((B + 1) * 4));
+  s.from = reinterpret_cast<int32_t*>(take(B * 4));
+  s.group_of = reinterpret_cast<int32_t*>(take(B * 4));
+  s.request_of_row = reinterpret_cast<int32_t*>(take((size_t)x.T * 4));
+  s.group = reinterpret_cast<Group*>(take(G * sizeof(Group)));
+  for (int i = 0; i < 2; ++i) {
+    const Shape sh = i == 0 ? prefix_shape(a) : shape_of(&x);
+    const size_t slots = 2 * (size_t)blocks_of(sh, x.cache.D) * rows_of(sh);
+    s.part_ml[i] = reinterpret_cast<float2*>(take(slots * 8));
+    s.part[i] = reinterpret_cast<float*>(take(slots * D * 4));
+    s.whole_ml[i] = reinterpret_cast<float2*>(take(rows * 8));
+    s.whole[i] = reinterpret_cast<float*>(take(rows * D * 4));
+  }
+  *bytes = off;
+  return s;
+}
+
+template <class T, int D, Kind kKind>
+hipError_t launch_kind(Shape sh, const GroupedParams& p, const tg_tree_attn_args* a, hipStream_t s) {
+  if (sh.q == 1)
+    return sh.shared ? launch_items<T, D, 1, true, kKind>(p, a, s)
+                     : launch_items<T, D, 1, false, kKind>(p, a, s);
+  if constexpr (D < 256)
+    return sh.shared ? launch_items<T, D, 2, true, kKind>(p, a, s)
+                     : launch_items<T, D, 2, false, kKind>(p, a, s);
+  return hipErrorInvalidValue;  // shape_for() gives no other
+}
+
+template <class T, int D>
+hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
+  const tg_tree_attn_args& x = a->attn;
+  const tg_kv_cache& c = x.cache;
+  const Shape shapes[2] = {prefix_shape(a), shape_of(&x)};
+  size_t bytes;
+  const Space sp = carve(a, static_cast<char*>(ws), &bytes);
+  const int cap = c.max_pages * c.page_size;
+  PlanParams plan;
+  plan.B = c.B;
+  plan.groups = a->n_groups;
+  plan.T = x.T;
+  plan.max_nodes = x.max_nodes;
+  plan.cap = cap;
+  plan.G = x.Hq / c.Hkv;
+  plan.Hkv = c.Hkv;
+  plan.prefix_rows = rows_of(shapes[0]);
+  plan.prefix_unit = unit_of(shapes[0]);
+  plan.tail_rows = rows_of(shapes[1]);
+  plan.tail_unit = unit_of(shapes[1]);
+  plan.off = x.q_offsets;
+  plan.lengths = x.lengths;
+  plan.group_off = a->group_offsets;
+  plan.shared = a->shared;
+  plan.pre_prefix = sp.pre_prefix;
+  plan.pre_tail = sp.pre_tail;
+  plan.from = sp.from;
+  plan.group_of = sp.group_of;
+  plan.request_of_row = sp.request_of_row;
+  plan.group = sp.group;
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanBlock), 0, s, plan);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  JoinParams j;
+  GroupedParams p;
+  fill(&p, &x);
+  p.split = nullptr;
+  p.from = sp.from;
+  p.groups = sp.group;
+  for (int i = 0; i < 2; ++i) {
+    p.pre = i ? sp.pre_tail : sp.pre_prefix;
+    p.part = sp.part[i];
+    p.part_ml = sp.part_ml[i];
+    p.whole = sp.whole[i];
+    p.whole_ml = sp.whole_ml[i];
+    p.B = i ? c.B : a->n_groups;
+    Parts& q = i ? j.tail : j.prefix;
+    q = {p.pre, p.part, p.part_ml, p.whole, p.whole_ml, rows_of(shapes[i]), unit_of(shapes[i]),
+         blocks_of(shapes[i], D)};
+    if (p.B == 0) continue;
+    e = i ? launch_kind<T, D, kTail>(shapes[i], p, &x, s)
+          : launch_kind<T, D, kPrefix>(shapes[i], p, &x, s);
+    if (e != hipSuccess) return e;
+  }
+  j.off = x.q_offsets;
+  j.lengths = x.lengths;
+  j.from = sp.from;
+  j.group_of = sp.group_of;
+  j.request_of_row = sp.request_of_row;
+  j.group = sp.group;
+  j.out = p.out;
+  j.out_stride = p.out_stride;
+  j.T = x.T;
+  j.Hkv = c.Hkv;
+  j.G = p.G;
+  j.cap = cap;
+  j.max_nodes = x.max_nodes;
+  j.B = c.B;
+  j.groups = a->n_groups;
+  constexpr int kHeads = kWaves * (kWave / (D / 4));  // per block
+  hipLaunchKernelGGL((join_parts_kernel<T, D>), dim3(x.T, (x.Hq + kHeads - 1) / kHeads), dim3(kBlock),
+                     0, s, j);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_type(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
+  switch (a->attn.cache.D) {
+    case 64: return launch<T, 64>(a, ws, s);
+    case 128: return launch<T, 128>(a, ws, s);
+    default: return launch<T, 256>(a, ws, s);
+  }
+}
+
+}  // namespace
+
+size_t prefix_attention_workspace_bytes(const tg_prefix_attn_args* a) {
+  size_t bytes;
+  carve(a, nullptr, &bytes);
+  return bytes;
+}
+
+hipError_t launch_prefix_attention(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
+  if (a->attn.T == 0 || a->attn.cache.B == 0) return hipSuccess;
+  return a->attn.cache.dtype == TG_BF16 ? launch_type<Bf16>(a, ws, s) : launch_type<F16>(a, ws, s);
+}
+
+}  // namespace tg

@@ -768,6 +768,7 @@ __device__ __forceinline__ void settle_picked(DrawShared& sh, const Weigh& weigh
   const bool stays = w && nb < most && mb < mass;
   u64 least = stays ? key : ~0ull;
   for (int o = 1; o < kWave; o *= 2) least = min(least, shfl_xor64(least, o));
+  if (least == ~0ull) least = cut;  // the border is among tokens without weight
   const u64 sum = wave_sum(stays ? w : 0);
   if (lane == 0) {
     sh.key = least;

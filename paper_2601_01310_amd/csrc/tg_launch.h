@@ -144,6 +144,8 @@ hipError_t launch_kv_restore(const void* store, size_t store_bytes, const uint64
 hipError_t launch_qk_norm_rope(const tg_qk_args* a, hipStream_t stream);
 size_t tree_attention_workspace_bytes(const tg_tree_attn_args* a);
 hipError_t launch_tree_attention(const tg_tree_attn_args* a, void* ws, hipStream_t stream);
+size_t prefix_attention_workspace_bytes(const tg_prefix_attn_args* a);
+hipError_t launch_prefix_attention(const tg_prefix_attn_args* a, void* ws, hipStream_t stream);
 size_t verify_workspace_bytes(const tg_verify_args* a);
 hipError_t launch_verify_tree(const tg_verify_args* a, void* ws, hipStream_t stream);
 size_t sample_workspace_bytes(const tg_sample_args* a);

@@ -226,6 +226,33 @@ def _mask(tree_mask, T) -> int:
     return tree_mask.shape[1]
 
 
+def _attention(a, cache: KvCache, q, q_offsets, lengths, tree_mask, scale, max_nodes, out):
+    """Checks the tensors of an attention call and puts them into its arguments;
+    returns ``out``."""
+    c, dtype = cache.args, cache.k.dtype
+    T, Hq = q.shape[0], q.shape[1]
+    stride = _rows(q, "q", dtype, (Hq, c.D))
+    if out is None:
+        out = torch.empty((T, Hq, c.D), dtype=dtype, device=q.device)
+    out_stride = _rows(out, "out", dtype, (Hq, c.D))
+    if out.shape[0] != T:
+        raise ValueError(f"out has {out.shape[0]} rows, {T} required")
+    _want(q_offsets, "q_offsets", torch.int32, (c.B + 1,))
+    _want(lengths, "lengths", torch.int32, (c.B,))
+    words = _mask(tree_mask, T)
+    _same_device(cache.k, q, out, q_offsets, lengths, tree_mask)
+    if max_nodes is None:
+        max_nodes = max(1, min(T, tg.MAX_NODES, 64 * words if words else tg.MAX_NODES))
+        a.typical_nodes = -(-T // max(1, c.B))
+    a.cache, a.T, a.Hq, a.max_nodes, a.mask_words = c, T, Hq, max_nodes, words
+    a.scale = 1.0 / math.sqrt(c.D) if scale is None else scale
+    a.q_stride, a.out_stride = stride, out_stride
+    for name, t in dict(q=q, q_offsets=q_offsets, lengths=lengths, tree_mask=tree_mask,
+                        out=out).items():
+        setattr(a, name, None if t is None else t.data_ptr())
+    return out
+
+
 class TreeAttention:
     """Attention of ``q`` [T, Hq, D] over the cache; returns ``out`` (a tensor
     of its own if not given). ``tree_mask`` [T, W] int64 (the bits of tg.h's
@@ -235,30 +262,9 @@ class TreeAttention:
 
     def __init__(self, cache: KvCache, q, q_offsets, lengths, tree_mask=None, scale=None,
                  max_nodes=None, out=None):
-        c, dtype = cache.args, cache.k.dtype
-        T, Hq = q.shape[0], q.shape[1]
-        stride = _rows(q, "q", dtype, (Hq, c.D))
-        if out is None:
-            out = torch.empty((T, Hq, c.D), dtype=dtype, device=q.device)
-        out_stride = _rows(out, "out", dtype, (Hq, c.D))
-        if out.shape[0] != T:
-            raise ValueError(f"out has {out.shape[0]} rows, {T} required")
-        _want(q_offsets, "q_offsets", torch.int32, (c.B + 1,))
-        _want(lengths, "lengths", torch.int32, (c.B,))
-        words = _mask(tree_mask, T)
-        _same_device(cache.k, q, out, q_offsets, lengths, tree_mask)
         a = self.args = tg.TreeAttnArgs()
-        if max_nodes is None:
-            max_nodes = max(1, min(T, tg.MAX_NODES, 64 * words if words else tg.MAX_NODES))
-            a.typical_nodes = -(-T // max(1, c.B))
+        self.out = _attention(a, cache, q, q_offsets, lengths, tree_mask, scale, max_nodes, out)
         self._keep = (cache, q, q_offsets, lengths, tree_mask)
-        self.out = out
-        a.cache, a.T, a.Hq, a.max_nodes, a.mask_words = c, T, Hq, max_nodes, words
-        a.scale = 1.0 / math.sqrt(c.D) if scale is None else scale
-        a.q_stride, a.out_stride = stride, out_stride
-        for name, t in dict(q=q, q_offsets=q_offsets, lengths=lengths, tree_mask=tree_mask,
-                            out=out).items():
-            setattr(a, name, None if t is None else t.data_ptr())
         self.ws_bytes = tg.tg_tree_attention_workspace(a)
         if self.ws_bytes == 0:
             raise tg.TgError(tg.load().tg_tree_attention(ctypes.byref(a), None, 0, None),
@@ -269,6 +275,38 @@ class TreeAttention:
 
     def __call__(self, layer=0, stream=None):
         self.args.layer = layer
+        _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
+        return self.out
+
+
+class PrefixAttention:
+    """:class:`TreeAttention` for groups of requests that share the pages of a
+    prefix (after :meth:`KvCache.fork`), which is read once for each group.
+    ``group_offsets`` [n + 1] int32: group g is the requests group_offsets[g] up
+    to group_offsets[g + 1]; ``shared`` [n] int32: the positions whose pages they
+    have in common. Both are read on the device at every call."""
+
+    def __init__(self, cache: KvCache, q, q_offsets, lengths, group_offsets, shared, tree_mask=None,
+                 scale=None, max_nodes=None, out=None):
+        a = self.args = tg.PrefixAttnArgs()
+        self.out = _attention(a.attn, cache, q, q_offsets, lengths, tree_mask, scale, max_nodes, out)
+        _want(shared, "shared", torch.int32, (None,))
+        n = shared.shape[0]
+        _want(group_offsets, "group_offsets", torch.int32, (n + 1,))
+        _same_device(q, group_offsets, shared)
+        a.n_groups = n
+        a.group_offsets, a.shared = group_offsets.data_ptr(), shared.data_ptr()
+        self._keep = (cache, q, q_offsets, lengths, tree_mask, group_offsets, shared)
+        self.ws_bytes = tg.tg_prefix_attention_workspace(a)
+        if self.ws_bytes == 0:
+            raise tg.TgError(tg.load().tg_prefix_attention(ctypes.byref(a), None, 0, None),
+                             "workspace")
+        self.ws = tg.workspace(self.ws_bytes, q.device)
+        self._ref, self._device, self._ws = ctypes.byref(a), q.get_device(), self.ws.data_ptr()
+        self._call = tg.load().tg_prefix_attention
+
+    def __call__(self, layer=0, stream=None):
+        self.args.attn.layer = layer
         _run(self._call, self._device, stream, self._ref, self._ws, self.ws_bytes)
         return self.out
 

@@ -25,7 +25,7 @@ EXPORTS = [
     "tg_ew_few_workspace", "tg_ew_few",
     "tg_ew_replay_workspace", "tg_ew_replay", "tg_batch_trigger", "tg_kv_checkpoint",
     "tg_kv_checkpoint_strided", "tg_kv_restore", "tg_qk_norm_rope", "tg_tree_attention_workspace",
-    "tg_tree_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_sample_workspace",
+    "tg_tree_attention", "tg_prefix_attention_workspace", "tg_prefix_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_sample_workspace",
     "tg_sample", "tg_kv_compact",
     "tg_kv_pages_reserve", "tg_kv_pages_fork", "tg_kv_pages_trim",
 ]
@@ -92,6 +92,12 @@ class TreeAttnArgs(ctypes.Structure):
         ("int", "layer T Hq max_nodes mask_words"), ("float", "scale"),
         ("i64", "q_stride out_stride"), ("ptr", "q q_offsets lengths tree_mask out"),
         ("int", "typical_nodes")])
+
+
+class PrefixAttnArgs(ctypes.Structure):
+    """Mirror of ``tg_prefix_attn_args``."""
+    _fields_ = [("attn", TreeAttnArgs)] + _fields([
+        ("int", "n_groups"), ("ptr", "group_offsets shared")])
 
 
 class VerifyArgs(ctypes.Structure):
@@ -170,7 +176,8 @@ def load(path: Optional[str] = None):
     kv = ctypes.POINTER(KvCacheArgs)
     lib.tg_qk_norm_rope.restype = i
     lib.tg_qk_norm_rope.argtypes = [ctypes.POINTER(QkArgs), vp]
-    for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_verify_tree", VerifyArgs),
+    for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_prefix_attention", PrefixAttnArgs),
+                       ("tg_verify_tree", VerifyArgs),
                        ("tg_sample", SampleArgs)):
         size, call = getattr(lib, name + "_workspace"), getattr(lib, name)
         size.restype, size.argtypes = sz, [ctypes.POINTER(args)]
@@ -351,6 +358,10 @@ def tg_kv_restore(store, store_bytes, commit, seq, src, dst, nbytes, n, kv_dst, 
 
 def tg_tree_attention_workspace(args: TreeAttnArgs) -> int:
     return int(load().tg_tree_attention_workspace(ctypes.byref(args)))
+
+
+def tg_prefix_attention_workspace(args: PrefixAttnArgs) -> int:
+    return int(load().tg_prefix_attention_workspace(ctypes.byref(args)))
 
 
 def tg_verify_tree_workspace(args: VerifyArgs) -> int:

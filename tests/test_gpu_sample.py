@@ -161,6 +161,18 @@ def test_ties(V, filters):
     check(make(*a), *a)
 
 
+def test_top_k_beyond_the_tokens_that_have_a_weight():
+    """Cold rows, most of whose tokens are too small to count."""
+    V = 9000
+    logits = torch.randn((6, V), generator=gen(4), device=DEV).mul_(4)
+    u = torch.rand(6, generator=gen(5), device=DEV)
+    hot = torch.tensor([0.05, 0.1, 0.02, 1e-3, 0.2, 0.3], device=DEV)
+    k = torch.tensor([500, 8999, 3000, 50, 2000, 4000], dtype=torch.int32, device=DEV)
+    for p in (None, torch.full((6,), 0.99, device=DEV)):
+        a = (logits, u, hot, k, p, None)
+        check(make(*a), *a)
+
+
 def test_rows_of_equal_logits_keep_the_first_ones():
     V = 6000
     logits = torch.full((2, V), 2.5, device=DEV)
