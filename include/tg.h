@@ -622,7 +622,7 @@ tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, voi
  * largest float32. A row without tokens gives -1. probs [T, V] float32 (NULL: not
  * wanted; rows probs_stride apart) gets w_i over the mass of all that stay, 0 for
  * the others, and 0 everywhere for a row without tokens. Limits: V <= 2^24,
- * T * ceil(V / 8192) < 2^31; logits aligned to their type.
+ * T * ceil(V / 4096) < 2^31; logits aligned to their type.
  */
 typedef struct {
   int dtype; /* of logits: TG_F32, TG_BF16 or TG_F16 */

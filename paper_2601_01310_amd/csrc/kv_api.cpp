@@ -185,7 +185,7 @@ tg_status check_sample(const tg_sample_args* a) {
   if (a->T < 0 || a->V <= 0)
     return set_error(TG_ERR_BAD_DIM, "T=%d must be >= 0 and V=%d > 0", a->T, a->V);
   if (a->V > (1 << 24)) return set_error(TG_ERR_UNSUPPORTED, "V=%d exceeds 2^24", a->V);
-  if ((long long)a->T * ((a->V + 8191) / 8192) >= (1LL << 31))  // blocks are counted in 32 bits
+  if ((long long)a->T * ((a->V + 4095) / 4096) >= (1LL << 31))  // blocks are counted in 32 bits
     return set_error(TG_ERR_UNSUPPORTED, "T=%d rows of %d logits are too many", a->T, a->V);
   if (a->logits_stride < a->V || (a->probs && a->probs_stride < a->V))
     return set_error(TG_ERR_BAD_DIM, "a row of logits or probabilities is longer than its stride");

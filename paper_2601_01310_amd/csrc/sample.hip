@@ -7,7 +7,7 @@
 // tokens coarsely: the borders of top-k and top-p each lie in one step (or, of
 // top-p within top-k, in a few), whose tokens alone have to be put in order.
 //
-//   part   8192 tokens a block, read once: their largest, the mass of every 1024,
+//   part   4096 tokens a block, read once: their largest, the mass of every 1024,
 //          and, for rows with filters, tokens and mass of every step;
 //   cut    a row's steps added up: those that hold the borders;
 //   keep   the logits again (from the last-level cache): the mass of every 1024 of
@@ -22,7 +22,7 @@
 namespace tg {
 namespace {
 
-constexpr int kPart = 8192, kPartBlock = 256, kPartWaves = kPartBlock / kWave;
+constexpr int kPart = 4096, kPartBlock = 256, kPartWaves = kPartBlock / kWave;
 constexpr int kChunk = 1024;  // tokens that a wave takes at a time
 constexpr int kEach = kChunk / kWave;
 constexpr int kMine = kPart / (kChunk * kPartWaves);  // chunks of a wave of a part
@@ -31,10 +31,10 @@ constexpr int kNone = kSteps - 1;  // what is too small for a weight
 constexpr int kBuckets = 1024;    // masses in token order, of the draw
 constexpr int kDigits = 2048;     // of the radix selection
 constexpr int kList = 3328;       // listed tokens of a row and border
-constexpr int kPartList = 1024;   // of a part
+constexpr int kPartList = 768;    // of a part
 constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / kWave;
 constexpr uint32_t kOverflow = 1u << 24;
-constexpr int kFoldParts = 4;
+constexpr int kFoldParts = 8;
 
 typedef unsigned long long u64;
 
@@ -422,7 +422,7 @@ struct CutShared {
   CutInfo c;
 };
 
-template <int kThreads>
+template <int kThreads, int kUnroll>
 __device__ __forceinline__ void find_cut(const Params& p, const Filters& f, int t, CutShared& sh) {
   constexpr int kPer = kSteps / kThreads, kWaves = kThreads / kWave;
   const int tid = threadIdx.x;
@@ -455,7 +455,7 @@ __device__ __forceinline__ void find_cut(const Params& p, const Filters& f, int 
       __syncthreads();
       sh.below[tid] = b ? (int)fmin(base - base_of(b, c64), 64.0) : 64;
       __syncthreads();
-#pragma unroll 4
+#pragma unroll kUnroll
       for (int i = 0; i < parts; ++i) {
         const int down = sh.below[i];
         const int64_t at = ((int64_t)t * p.parts + i0 + i) * kSteps;
@@ -525,7 +525,7 @@ __global__ __launch_bounds__(kSteps) void cut_kernel(const Params p) {
   const int t = blockIdx.x;
   const Filters f(p, t);
   if (f.greedy || !f.any()) return;
-  find_cut<kSteps>(p, f, t, sh);
+  find_cut<kSteps, 8>(p, f, t, sh);
   if (threadIdx.x == 0) p.sp.cut[t] = sh.c;
 }
 
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(kPartBlock) void keep_kernel(const uint8_t* __restr
   fill_table(table, p.s);
   if (tid < 2) n[tid] = 0;
   if constexpr (kFold) {
-    find_cut<kPartBlock>(p, f, t, cut);
+    find_cut<kPartBlock, 2>(p, f, t, cut);
     if (part == 0 && tid == 0) p.sp.cut[t] = cut.c;
   } else {
     if (tid == 0) cut.c = p.sp.cut[t];
@@ -936,7 +936,14 @@ __global__ __launch_bounds__(kDrawBlock) void draw_kernel(const uint8_t* __restr
       const uint32_t n = p.sp.listed[2 * t + round];
       __syncthreads();
       if (n <= kList)
-        for (uint32_t i = tid; i < n; i += kDrawBlock) sh.list[i] = from[i];
+        for (uint32_t i0 = tid; i0 < n; i0 += 8 * kDrawBlock) {
+          u64 x[8];  // loads together
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = from[min(i0 + j * kDrawBlock, n - 1)];
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (i0 + j * kDrawBlock < n) sh.list[i0 + j * kDrawBlock] = x[j];
+        }
       __syncthreads();
       const Border<T> border{row, weigh, sh.list, n, round ? c.p_lo : c.k_step,
                              round ? c.p_hi : c.k_step};
@@ -1026,7 +1033,6 @@ __global__ __launch_bounds__(kPartBlock) void probs_kernel(const uint8_t* __rest
   const u64 floor_w = one ? 0 : weigh.floor_of(f, best);
   const double scale = one ? 0.0 : 1.0 / (double)c->whole;
   float* const probs = p.probs + (int64_t)t * p.probs_stride;
-  const bool wide = (reinterpret_cast<uintptr_t>(probs) & 15) == 0;
 #pragma unroll
   for (int j = 0; j < kMine; ++j)
 #pragma unroll
@@ -1047,8 +1053,8 @@ __global__ __launch_bounds__(kPartBlock) void probs_kernel(const uint8_t* __rest
           }
         }
       }
-      if (wide && i + 4 <= p.V) {
-        *reinterpret_cast<float4*>(probs + i) = make_float4(y[0], y[1], y[2], y[3]);
+      if (i + 4 <= p.V) {  // (rows are aligned to 4 bytes only)
+        __builtin_memcpy(probs + i, y, 16);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
