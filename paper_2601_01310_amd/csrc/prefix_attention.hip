@@ -241,6 +241,9 @@ Shape prefix_shape(const tg_prefix_attn_args* a) {
 }
 
 int blocks_of(Shape s, int D) { return kCus * occupancy(D, s.q); }
+int least_blocks(Shape s, Shape t, int D) {
+  return blocks_of(s, D) < blocks_of(t, D) ? blocks_of(s, D) : blocks_of(t, D);
+}
 
 struct Space {
   int32_t *pre_prefix, *pre_tail, *from, *group_of, *request_of_row;
@@ -277,11 +280,61 @@ Space carve(const tg_prefix_attn_args* a, char* base, size_t* bytes) {
   return s;
 }
 
+// Both in one launch, for tails of at most 16 rows a KV head: every other block
+// takes prefixes, which the products and the vector unit bound, or tails, which the
+// memory does, so that each CU has both at once.
+template <class T, int D, int kQ, bool kShared, int kPages, int kOcc>
+__global__ __launch_bounds__(kBlock, kOcc) void both_kernel(
+    const GroupedParams prefix, const GroupedParams tail, const int32_t* __restrict__ table,
+    const int32_t* __restrict__ off, const int32_t* __restrict__ lengths,
+    const uint64_t* __restrict__ mask) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const Blocks at_work = {(int)blockIdx.x / 2, (int)gridDim.x / 2, 4};
+  if (blockIdx.x % 2) {
+    split_items<T, D, 1, kPages, kTail>(tail, table, off, lengths, mask, smem, at_work);
+  } else if constexpr (kShared) {
+    constexpr int kTiles = 8 * kTile * D * 2;  // bytes
+    shared_items<T, D, kQ, kPages != 0, kPrefix>(prefix, table, off, lengths, mask,
+                                                 reinterpret_cast<uint16_t*>(smem),
+                                                 reinterpret_cast<int*>(smem + kTiles), at_work);
+  } else {
+    split_items<T, D, kQ, kPages, kPrefix>(prefix, table, off, lengths, mask, smem, at_work);
+  }
+}
+
+bool merged(const tg_prefix_attn_args* a) {
+  const Shape tail = shape_of(&a->attn);
+  return tail.q == 1 && !tail.shared;
+}
+
+template <class T, int D, int kQ, bool kShared>
+hipError_t launch_both(const GroupedParams& prefix, const GroupedParams& tail,
+                       const tg_tree_attn_args* a, hipStream_t s) {
+  constexpr int kOcc = occupancy(D, kQ) < occupancy(D, 1) ? occupancy(D, kQ) : occupancy(D, 1);
+  const tg_kv_cache& c = a->cache;
+  const size_t one = (kShared ? (size_t)8 * kTile * D * 2 : split_lds<T, D, kQ>()) + (prefix.B + 1) * 4;
+  const size_t two = split_lds<T, D, 1>() + (tail.B + 1) * 4, lds = one > two ? one : two;
+  auto go = [&](auto* kernel) -> hipError_t {
+    if (lds > 48 * 1024) {
+      const hipError_t e =
+          hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3(2 * kCus * kOcc), dim3(kBlock), lds, s, prefix, tail,
+                       c.page_table, a->q_offsets, a->lengths, a->tree_mask);
+    return hipGetLastError();
+  };
+  return c.page_size >= kTile       ? go(both_kernel<T, D, kQ, kShared, 1, kOcc>)
+         : c.page_size == kTile / 2 ? go(both_kernel<T, D, kQ, kShared, 2, kOcc>)
+                                    : go(both_kernel<T, D, kQ, kShared, 0, kOcc>);
+}
+
 template <class T, int D, Kind kKind>
 hipError_t launch_kind(Shape sh, const GroupedParams& p, const tg_tree_attn_args* a, hipStream_t s) {
-  if (sh.q == 1)
-    return sh.shared ? launch_items<T, D, 1, true, kKind>(p, a, s)
-                     : launch_items<T, D, 1, false, kKind>(p, a, s);
+  if (sh.q == 1 && sh.shared) return launch_items<T, D, 1, true, kKind>(p, a, s);
+  if constexpr (kKind == kPrefix)  // (such tails go by launch_both)
+    if (sh.q == 1) return launch_items<T, D, 1, false, kKind>(p, a, s);
   if constexpr (D < 256)
     return sh.shared ? launch_items<T, D, 2, true, kKind>(p, a, s)
                      : launch_items<T, D, 2, false, kKind>(p, a, s);
@@ -322,12 +375,14 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   JoinParams j;
-  GroupedParams p;
-  fill(&p, &x);
-  p.split = nullptr;
-  p.from = sp.from;
-  p.groups = sp.group;
+  GroupedParams both[2];
+  const bool merge = merged(a);
   for (int i = 0; i < 2; ++i) {
+    GroupedParams& p = both[i];
+    fill(&p, &x);
+    p.split = nullptr;
+    p.from = sp.from;
+    p.groups = sp.group;
     p.pre = i ? sp.pre_tail : sp.pre_prefix;
     p.part = sp.part[i];
     p.part_ml = sp.part_ml[i];
@@ -336,10 +391,21 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
     p.B = i ? c.B : a->n_groups;
     Parts& q = i ? j.tail : j.prefix;
     q = {p.pre, p.part, p.part_ml, p.whole, p.whole_ml, rows_of(shapes[i]), unit_of(shapes[i]),
-         blocks_of(shapes[i], D)};
-    if (p.B == 0) continue;
+         merge ? least_blocks(shapes[0], shapes[1], D) : blocks_of(shapes[i], D)};
+    if (p.B == 0 || merge) continue;
     e = i ? launch_kind<T, D, kTail>(shapes[i], p, &x, s)
           : launch_kind<T, D, kPrefix>(shapes[i], p, &x, s);
+    if (e != hipSuccess) return e;
+  }
+  if (merge) {
+    const Shape sh = shapes[0];
+    e = hipErrorInvalidValue;  // shape_for() gives no other
+    if (sh.q == 1)
+      e = sh.shared ? launch_both<T, D, 1, true>(both[0], both[1], &x, s)
+                    : launch_both<T, D, 1, false>(both[0], both[1], &x, s);
+    else if constexpr (D < 256)
+      e = sh.shared ? launch_both<T, D, 2, true>(both[0], both[1], &x, s)
+                    : launch_both<T, D, 2, false>(both[0], both[1], &x, s);
     if (e != hipSuccess) return e;
   }
   j.off = x.q_offsets;
@@ -348,11 +414,11 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
   j.group_of = sp.group_of;
   j.request_of_row = sp.request_of_row;
   j.group = sp.group;
-  j.out = p.out;
-  j.out_stride = p.out_stride;
+  j.out = both[1].out;
+  j.out_stride = x.out_stride;
   j.T = x.T;
   j.Hkv = c.Hkv;
-  j.G = p.G;
+  j.G = both[1].G;
   j.cap = cap;
   j.max_nodes = x.max_nodes;
   j.B = c.B;

@@ -198,6 +198,12 @@ struct Piece {
   bool whole;
 };
 
+// Which of `all` blocks this one is; neighbours lie on `xcds` XCDs in turn.
+struct Blocks {
+  int block, all, xcds;
+};
+__device__ __forceinline__ Blocks whole_grid() { return {(int)blockIdx.x, (int)gridDim.x, 8}; }
+
 // Deals the units to the blocks in runs of one length; the units before each request
 // are kept in LDS. Up to 64 requests are summed in the lanes of each wave, so
 // that the first piece needs one round of loads.
@@ -207,16 +213,17 @@ struct Dealer {
   const int32_t* __restrict__ off;
   const int32_t* __restrict__ lengths;
   int* pre;  // LDS, [B + 1]
+  Blocks at_work;
   int begin, stop, share, me;
 
   __device__ __forceinline__ Dealer(const ParamsOf<kKind>& p_, const int32_t* __restrict__ off_,
-                                    const int32_t* __restrict__ lengths_, int* pre_)
-      : p(p_), off(off_), lengths(lengths_), pre(pre_) {}
+                                    const int32_t* __restrict__ lengths_, int* pre_, Blocks at_work_)
+      : p(p_), off(off_), lengths(lengths_), pre(pre_), at_work(at_work_) {}
 
   __device__ __forceinline__ void runs(int total) {
-    const int blocks = gridDim.x;
+    const int blocks = at_work.all, x = at_work.xcds;
     // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
-    me = (blockIdx.x % 8) * (blocks / 8) + blockIdx.x / 8;
+    me = (at_work.block % x) * (blocks / x) + at_work.block / x;
     share = max(1, (total + blocks - 1) / blocks);
     begin = (int)min((int64_t)total, (int64_t)me * share);
     stop = min(total, begin + share);
@@ -332,7 +339,7 @@ struct Dealer {
     Split s;
     const int start = unit - x.u0;  // the item's first unit
     s.k0 = start / share;
-    s.parts = min((start + x.r.units - 1) / share, (int)gridDim.x - 1) - s.k0 + 1;
+    s.parts = min((start + x.r.units - 1) / share, at_work.all - 1) - s.k0 + 1;
     s.at = me - s.k0;
     s.slot = start == s.k0 * share ? 0 : 1;
     s.first = x.r.first;
@@ -516,16 +523,18 @@ struct Rows {
 
 // kPages: pages per tile, 1 (pages of 32 rows and more) or 2 (of 16), whose
 // addresses are the wave's; 0: smaller ones, an address per lane.
-template <class T, int D, int kQ, int kPages, int kOcc, Kind kKind>
-__global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
-    const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
-    const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+template <class T, int D, int kQ, int kPages, Kind kKind>
+__device__ __forceinline__ void split_items(const ParamsOf<kKind>& p,
+                                            const int32_t* __restrict__ table,
+                                            const int32_t* __restrict__ off,
+                                            const int32_t* __restrict__ lengths,
+                                            const uint64_t* __restrict__ mask, char* smem,
+                                            Blocks at_work) {
   using R = Rows<T, D, kQ>;
   constexpr int kRows = 16 * kQ, kUnit = kWaves * kTile;
   constexpr int kLanes = D / 8;         // lanes that load a row of V
   constexpr int kPer = kWave / kLanes;  // rows of V per load
   constexpr int kLoads = kTile / kPer;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int carry[kWaves];
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
@@ -533,7 +542,7 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
   float2* const ml = reinterpret_cast<float2*>(smem + kWaves * kTile * R::kPitch * 2);
   int* const pre = reinterpret_cast<int*>(ml + kWaves * kRows);
 
-  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre);
+  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre, at_work);
   Piece x = run.first(carry);
   if (run.begin >= run.stop) {
     run.leave_none();
@@ -742,6 +751,18 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
   }
 }
 
+template <class T, int D, int kQ, int kPages, int kOcc, Kind kKind>
+__global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
+    const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
+    const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  split_items<T, D, kQ, kPages, kKind>(p, table, off, lengths, mask, smem, whole_grid());
+}
+template <class T, int D, int kQ>
+constexpr size_t split_lds() {
+  return (size_t)kWaves * kTile * Rows<T, D, kQ>::kPitch * 2 + kWaves * 16 * kQ * 8;
+}
+
 // The four waves take kQ groups of 16 rows each and share tiles of 64
 // positions, which go straight from the cache into one of two LDS buffers
 // (no registers, no LDS instructions) while the other is multiplied. A row of
@@ -750,26 +771,27 @@ __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
 // banks, as rows of other lengths would do, which these loads cannot write.
 // kEven: a page holds the rows that a wave loads at once, whose address is the
 // wave's then.
-template <class T, int D, int kQ, bool kEven, int kOcc, Kind kKind>
-__global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
-    const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
-    const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+template <class T, int D, int kQ, bool kEven, Kind kKind>
+__device__ __forceinline__ void shared_items(const ParamsOf<kKind>& p,
+                                             const int32_t* __restrict__ table,
+                                             const int32_t* __restrict__ off,
+                                             const int32_t* __restrict__ lengths,
+                                             const uint64_t* __restrict__ mask, uint16_t* tiles,
+                                             int* pre, Blocks at_work) {
   using R = Rows<T, D, kQ>;
   constexpr int kRows = 16 * kQ * kWaves, kUnit = 2 * kTile;
   constexpr int kLanes = D / 8;            // lanes per row
   constexpr int kHave = kWave / kLanes;    // rows per load of a wave
   constexpr int kLoads = kUnit / (kHave * kWaves);
   constexpr int kTileElems = kUnit * D;
-  // [buffer][K, V][kUnit][D]
-  __shared__ __attribute__((aligned(16))) uint16_t tiles[4 * kTileElems];
-  extern __shared__ __attribute__((aligned(16))) int pre[];
+  // tiles: [buffer][K, V][kUnit][D]
   __shared__ int carry[kWaves];
   __shared__ uint32_t odd_rows[3][2];  // of the tiles, in turn
   const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
   const int col = lane & 15, quad = lane >> 4;
   auto turn_of = [](int row) { return (D == 64 ? row >> 1 & 3 : row & 7) * 2; };
 
-  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre);
+  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre, at_work);
   Piece x = run.first(carry);
   if (run.begin >= run.stop) {
     run.leave_none();
@@ -955,6 +977,15 @@ __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
   }
 }
 
+template <class T, int D, int kQ, bool kEven, int kOcc, Kind kKind>
+__global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
+    const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
+    const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+  __shared__ __attribute__((aligned(16))) uint16_t tiles[8 * kTile * D];
+  extern __shared__ __attribute__((aligned(16))) int pre[];
+  shared_items<T, D, kQ, kEven, kKind>(p, table, off, lengths, mask, tiles, pre, whole_grid());
+}
+
 // Which kernel: the rows of one KV head that requests have (at most, or as a
 // caller who cannot say so expects), over 16-row groups. Up to 32 rows
 // the split kernel reads the cache once per item; above, tiles of 64 rows in a
@@ -1016,7 +1047,6 @@ inline void fill(Params* p, const tg_tree_attn_args* a) {
 template <class T, int D, int kQ, bool kShared, Kind kKind>
 hipError_t launch_items(const ParamsOf<kKind>& p, const tg_tree_attn_args* a, hipStream_t s) {
   constexpr int kOcc = occupancy(D, kQ);
-  constexpr int kRows = rows_of(Shape{kQ, kShared});
   const tg_kv_cache& c = a->cache;
   auto go = [&](auto* kernel, size_t lds) -> hipError_t {
     if (lds > 64 * 1024) {
@@ -1034,7 +1064,7 @@ hipError_t launch_items(const ParamsOf<kKind>& p, const tg_tree_attn_args* a, hi
     return c.page_size >= 512 / D ? go(shared_kernel<T, D, kQ, true, kOcc, kKind>, pre)
                                   : go(shared_kernel<T, D, kQ, false, kOcc, kKind>, pre);
   } else {
-    const size_t lds = (size_t)kWaves * kTile * Rows<T, D, kQ>::kPitch * 2 + kWaves * kRows * 8 + pre;
+    const size_t lds = split_lds<T, D, kQ>() + pre;
     return c.page_size >= kTile       ? go(split_kernel<T, D, kQ, 1, kOcc, kKind>, lds)
            : c.page_size == kTile / 2 ? go(split_kernel<T, D, kQ, 2, kOcc, kKind>, lds)
                                       : go(split_kernel<T, D, kQ, 0, kOcc, kKind>, lds);
