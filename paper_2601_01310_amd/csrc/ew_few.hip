@@ -25,7 +25,15 @@ constexpr int kTableInts = 2048;  // a routing table up to this size is kept in 
 constexpr int kStep = 128;     // bytes of a weight row per step
 constexpr int kStage = 16 * kStep / 2;  // 16-bit elements of 16 rows' step in LDS
 constexpr int kGateLogits = 64;  // a block forms up to so many logits itself
-constexpr int kFusedTokens = 4;  // up to so many, the second kernel forms the sums
+// Up to so many tokens the second kernel forms the sums, with runs of 16 weight rows;
+// above, a third one does, and runs may be taller. 16 tokens of a Mixtral layer in 8
+// bits take 273 us the first way and 259 the second, 8 tokens 264 and 268, of a
+// DeepSeek-V3 share 86 and 93; in bf16 the first is the faster one up to 16 tokens
+// (share 205 and 208 us).
+template <bool kF8>
+constexpr int fused_tokens() {
+  return kF8 ? 8 : 16;
+}
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -355,6 +363,7 @@ __device__ __forceinline__ void topk(const float* lg, int E, int k, int t, int32
   else quick_topk<16>(lg, E, k, t, ids, w);
 }
 
+template <bool kFused>
 __device__ __forceinline__ void route(const Params& p, const int32_t* __restrict__ ert,
                                       const uint8_t* __restrict__ alive, Tables& tab, Route& r) {
   const int tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
@@ -408,8 +417,7 @@ __device__ __forceinline__ void route(const Params& p, const int32_t* __restrict
       used += __builtin_popcountll(__ballot(c > 0));
     }
     for (int o = 1; o < kWave; o *= 2) most = max(most, __shfl_xor(most, o));
-    const bool fused = p.T <= kFusedTokens;
-    const int group = most > kCols && !fused ? 2 * kCols : kCols;
+    const int group = most > kCols && !kFused ? 2 * kCols : kCols;
     int rows = 0, items = 0;
     for (int s0 = 0; s0 < p.S; s0 += kWave) {
       const int s = s0 + lane, c = count(s), m = (c + group - 1) / group;
@@ -430,7 +438,7 @@ __device__ __forceinline__ void route(const Params& p, const int32_t* __restrict
     }
     if (lane == 0) {
       r.n_items = items;
-      r.shape = fused            ? kNarrow
+      r.shape = kFused           ? kNarrow
                 : most > kCols    ? kWide
                 : rows > 2 * used ? kTall
                                   : kNarrow;
@@ -502,7 +510,7 @@ __global__ __launch_bounds__(kBlock, 2) void few_up_kernel(const Params p,
   float* const sums = reinterpret_cast<float*>(smem + kRingBytes);
   Route& r = *reinterpret_cast<Route*>(smem + kRingBytes + kPartsBytes);
   const int tid = threadIdx.x;
-  route(p, ert, alive, *reinterpret_cast<Tables*>(smem), r);
+  route<kFused>(p, ert, alive, *reinterpret_cast<Tables*>(smem), r);
   if (blockIdx.x == 0) {
     if (tid < p.P) {
       if (p.logits || p.w_gate) {
@@ -593,8 +601,8 @@ template <bool kF8>
 __global__ __launch_bounds__(kBlock, 4) void few_down_kernel(const Params p) {
   extern __shared__ __attribute__((aligned(16))) uint16_t ring[];
   __shared__ __attribute__((aligned(16))) float sums[2 * kWaves * kCols * 16];
-  __shared__ float y[kFusedTokens * 32][16];
   __shared__ Batch s;
+  float(*const y)[16] = reinterpret_cast<float(*)[16]>(ring + kWaves * kFusedRing * kStage);  // [T * k]
   const int tid = threadIdx.x;
   load_batch(p, s);
   const int tiles = p.d / 16, grid = gridDim.x, n = s.n_items;
@@ -673,9 +681,12 @@ struct Layout {
   size_t bytes;
 };
 
-bool fused(const tg_ew_args* a) { return a->T <= kFusedTokens; }
+bool fused(const tg_ew_few_args* a) {
+  return a->ew.T <= (a->weights == TG_WEIGHTS_F8 ? fused_tokens<true>() : fused_tokens<false>());
+}
 
-Layout layout(const tg_ew_args* a, char* base) {
+Layout layout(const tg_ew_few_args* few, char* base) {
+  const tg_ew_args* const a = &few->ew;
   size_t off = 0;
   const size_t np = (size_t)a->T * a->k;
   auto take = [&](size_t n) -> char* {
@@ -690,7 +701,7 @@ Layout layout(const tg_ew_args* a, char* base) {
   L.plan.w = reinterpret_cast<float*>(take(np * 4));
   L.plan.pairs = reinterpret_cast<uint16_t*>(take(np * 2));
   L.plan.h = reinterpret_cast<uint16_t*>(take(np * a->I * 2));
-  L.plan.y = reinterpret_cast<float*>(take(fused(a) ? 0 : np * a->d * 4));
+  L.plan.y = reinterpret_cast<float*>(take(fused(few) ? 0 : np * a->d * 4));
   L.ids = reinterpret_cast<int32_t*>(take(np * 4));
   L.bytes = off;
   return L;
@@ -711,7 +722,7 @@ hipError_t launch(const Params& p, const tg_ew_args& e, hipStream_t s) {
                      e.ert, e.slot_alive);
   if ((err = hipGetLastError()) != hipSuccess || e.T == 0) return err;
   if (kFused) {
-    const size_t lds = (size_t)kWaves * kFusedRing * kStage * 2;
+    const size_t lds = (size_t)kWaves * kFusedRing * kStage * 2 + (size_t)p.P * 16 * 4;
     if ((err = more_lds(few_down_kernel<kF8>, lds)) != hipSuccess) return err;
     const int tiles = p.d / 16;
     hipLaunchKernelGGL((few_down_kernel<kF8>), dim3(tiles < 2 * kCus ? tiles : 2 * kCus),
@@ -728,11 +739,11 @@ hipError_t launch(const Params& p, const tg_ew_args& e, hipStream_t s) {
 
 }  // namespace
 
-size_t ew_few_workspace_bytes(const tg_ew_few_args* a) { return layout(&a->ew, nullptr).bytes; }
+size_t ew_few_workspace_bytes(const tg_ew_few_args* a) { return layout(a, nullptr).bytes; }
 
 hipError_t launch_ew_few(const tg_ew_few_args* a, void* ws, hipStream_t s) {
   const tg_ew_args& e = a->ew;
-  Layout L = layout(&e, static_cast<char*>(ws));
+  Layout L = layout(a, static_cast<char*>(ws));
   Params p{};
   p.T = e.T, p.d = e.d, p.E = e.E, p.k = e.k, p.I = e.I, p.S = e.S, p.R = e.R, p.P = e.T * e.k;
   p.x = e.x;
@@ -764,8 +775,8 @@ hipError_t launch_ew_few(const tg_ew_few_args* a, void* ws, hipStream_t s) {
     p.ids = ids;
   }
   if (a->weights == TG_WEIGHTS_F8)
-    return fused(&e) ? launch<true, true>(p, e, s) : launch<true, false>(p, e, s);
-  return fused(&e) ? launch<false, true>(p, e, s) : launch<false, false>(p, e, s);
+    return fused(a) ? launch<true, true>(p, e, s) : launch<true, false>(p, e, s);
+  return fused(a) ? launch<false, true>(p, e, s) : launch<false, false>(p, e, s);
 }
 
 }  // namespace tg
