@@ -283,22 +283,31 @@ Space carve(const tg_prefix_attn_args* a, char* base, size_t* bytes) {
 // Both in one launch, for tails of at most 16 rows a KV head: every other block
 // takes prefixes, which the products and the vector unit bound, or tails, which the
 // memory does, so that each CU has both at once.
-template <class T, int D, int kQ, bool kShared, int kPages, int kOcc>
+template <class T, int D, int kPrefixQ, bool kShared, int kPagesOf, int kOcc>
 __global__ __launch_bounds__(kBlock, kOcc) void both_kernel(
     const GroupedParams prefix, const GroupedParams tail, const int32_t* __restrict__ table,
     const int32_t* __restrict__ off, const int32_t* __restrict__ lengths,
     const uint64_t* __restrict__ mask) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const Blocks at_work = {(int)blockIdx.x / 2, (int)gridDim.x / 2, 4};
+  using Grid = HalfGrid;
   if (blockIdx.x % 2) {
-    split_items<T, D, 1, kPages, kTail>(tail, table, off, lengths, mask, smem, at_work);
+    constexpr Kind kKind = kTail;
+    constexpr int kQ = 1, kPages = kPagesOf;
+    const GroupedParams& p = tail;
+#include "tg_attn_split.h"
   } else if constexpr (kShared) {
-    constexpr int kTiles = 8 * kTile * D * 2;  // bytes
-    shared_items<T, D, kQ, kPages != 0, kPrefix>(prefix, table, off, lengths, mask,
-                                                 reinterpret_cast<uint16_t*>(smem),
-                                                 reinterpret_cast<int*>(smem + kTiles), at_work);
+    constexpr Kind kKind = kPrefix;
+    constexpr int kQ = kPrefixQ;
+    constexpr bool kEven = kPagesOf != 0;
+    const GroupedParams& p = prefix;
+    uint16_t* const tiles = reinterpret_cast<uint16_t*>(smem);
+    int* const pre = reinterpret_cast<int*>(smem + 8 * kTile * D * 2);
+#include "tg_attn_shared.h"
   } else {
-    split_items<T, D, kQ, kPages, kPrefix>(prefix, table, off, lengths, mask, smem, at_work);
+    constexpr Kind kKind = kPrefix;
+    constexpr int kQ = kPrefixQ, kPages = kPagesOf;
+    const GroupedParams& p = prefix;
+#include "tg_attn_split.h"
   }
 }
 

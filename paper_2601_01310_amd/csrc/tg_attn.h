@@ -198,32 +198,38 @@ struct Piece {
   bool whole;
 };
 
-// Which of `all` blocks this one is; neighbours lie on `xcds` XCDs in turn.
-struct Blocks {
-  int block, all, xcds;
+// The blocks that work is dealt to: those of the grid, or every other one of them.
+// Neighbours lie on kXcds XCDs in turn.
+struct WholeGrid {
+  static constexpr uint32_t kXcds = 8;
+  static __device__ __forceinline__ uint32_t block() { return blockIdx.x; }
+  static __device__ __forceinline__ int blocks() { return (int)gridDim.x; }
 };
-__device__ __forceinline__ Blocks whole_grid() { return {(int)blockIdx.x, (int)gridDim.x, 8}; }
+struct HalfGrid {
+  static constexpr uint32_t kXcds = 4;
+  static __device__ __forceinline__ uint32_t block() { return blockIdx.x / 2; }
+  static __device__ __forceinline__ int blocks() { return (int)gridDim.x / 2; }
+};
 
 // Deals the units to the blocks in runs of one length; the units before each request
 // are kept in LDS. Up to 64 requests are summed in the lanes of each wave, so
 // that the first piece needs one round of loads.
-template <int kRows, int kUnit, Kind kKind>
+template <int kRows, int kUnit, Kind kKind, class Grid>
 struct Dealer {
   const ParamsOf<kKind>& p;
   const int32_t* __restrict__ off;
   const int32_t* __restrict__ lengths;
   int* pre;  // LDS, [B + 1]
-  Blocks at_work;
   int begin, stop, share, me;
 
   __device__ __forceinline__ Dealer(const ParamsOf<kKind>& p_, const int32_t* __restrict__ off_,
-                                    const int32_t* __restrict__ lengths_, int* pre_, Blocks at_work_)
-      : p(p_), off(off_), lengths(lengths_), pre(pre_), at_work(at_work_) {}
+                                    const int32_t* __restrict__ lengths_, int* pre_)
+      : p(p_), off(off_), lengths(lengths_), pre(pre_) {}
 
   __device__ __forceinline__ void runs(int total) {
-    const int blocks = at_work.all, x = at_work.xcds;
+    const int blocks = Grid::blocks();
     // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
-    me = (at_work.block % x) * (blocks / x) + at_work.block / x;
+    me = (Grid::block() % Grid::kXcds) * (blocks / (int)Grid::kXcds) + Grid::block() / Grid::kXcds;
     share = max(1, (total + blocks - 1) / blocks);
     begin = (int)min((int64_t)total, (int64_t)me * share);
     stop = min(total, begin + share);
@@ -339,7 +345,7 @@ struct Dealer {
     Split s;
     const int start = unit - x.u0;  // the item's first unit
     s.k0 = start / share;
-    s.parts = min((start + x.r.units - 1) / share, at_work.all - 1) - s.k0 + 1;
+    s.parts = min((start + x.r.units - 1) / share, Grid::blocks() - 1) - s.k0 + 1;
     s.at = me - s.k0;
     s.slot = start == s.k0 * share ? 0 : 1;
     s.first = x.r.first;
@@ -523,240 +529,13 @@ struct Rows {
 
 // kPages: pages per tile, 1 (pages of 32 rows and more) or 2 (of 16), whose
 // addresses are the wave's; 0: smaller ones, an address per lane.
-template <class T, int D, int kQ, int kPages, Kind kKind>
-__device__ __forceinline__ void split_items(const ParamsOf<kKind>& p,
-                                            const int32_t* __restrict__ table,
-                                            const int32_t* __restrict__ off,
-                                            const int32_t* __restrict__ lengths,
-                                            const uint64_t* __restrict__ mask, char* smem,
-                                            Blocks at_work) {
-  using R = Rows<T, D, kQ>;
-  constexpr int kRows = 16 * kQ, kUnit = kWaves * kTile;
-  constexpr int kLanes = D / 8;         // lanes that load a row of V
-  constexpr int kPer = kWave / kLanes;  // rows of V per load
-  constexpr int kLoads = kTile / kPer;
-  __shared__ int carry[kWaves];
-  const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
-  const int col = lane & 15, quad = lane >> 4;
-  uint16_t* const vt = reinterpret_cast<uint16_t*>(smem) + wave * kTile * R::kPitch;
-  float2* const ml = reinterpret_cast<float2*>(smem + kWaves * kTile * R::kPitch * 2);
-  int* const pre = reinterpret_cast<int*>(ml + kWaves * kRows);
-
-  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre, at_work);
-  Piece x = run.first(carry);
-  if (run.begin >= run.stop) {
-    run.leave_none();
-    return;
-  }
-  const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
-  for (int at = run.begin; at < run.stop;) {
-    if (at != run.begin) x = run.at(at);
-    run.leave(x, at);
-    const int32_t* __restrict__ pages = table + (int64_t)x.r.table * p.max_pages;
-    R rows;
-    rows.start(p, x, x.rt * kRows);
-
-    // The table's entry for position p0 + lane % 32 (kPages == 1: of the tile),
-    // and the page that it is, -1 for none: looked at only where it is used,
-    // since waiting for it means waiting for all loads before it.
-    auto entry_at = [&](int p0) -> int {
-      const int pos = kPages == 1 ? p0 : p0 + (lane & 31);
-      return pages[min(pos, x.r.end - 1) >> p.page_shift];
-    };
-    auto page_of = [&](int entry, int p0) -> int {
-      const int pos = kPages == 1 ? p0 : p0 + (lane & 31);
-      return pos < x.r.end && entry >= 0 && entry < p.n_pages ? entry : -1;
-    };
-    uint4 kn[2][R::kSteps], vn[kLoads];
-    // Loads of the tile at p0; positions without a page read page 0 and are
-    // masked.
-    const uint16_t* const kh = p.k + (int64_t)x.g * D;
-    const uint16_t* const vh = p.v + (int64_t)x.g * D;
-    auto load_tile = [&](int p0, int page) {
-      if (kPages) {
-        int64_t base[2];  // of the tile's halves
-        base[0] = (int64_t)uniform(max(page, 0)) * p.page_stride + (int64_t)(p0 & page_mask) * width;
-        base[1] = kPages == 1
-                      ? base[0] + 16 * width
-                      : (int64_t)max(__builtin_amdgcn_readlane(page, 16), 0) * p.page_stride;
-        const uint32_t kl = (col * width + quad * 8) * 2;
-        const uint32_t vl = (lane / kLanes * width + lane % kLanes * 8) * 2;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int s = 0; s < R::kSteps; ++s)
-            kn[t][s] = *reinterpret_cast<const uint4*>(
-                reinterpret_cast<const char*>(kh + base[t]) + s * 64 + kl);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-          vn[j] = *reinterpret_cast<const uint4*>(
-              reinterpret_cast<const char*>(vh + base[j / (kLoads / 2)] +
-                                            j % (kLoads / 2) * kPer * width) + vl);
-      } else {
-        auto row_of = [&](int row) -> int64_t {
-          const int pg = __shfl(page, row);
-          return pg < 0 ? 0 : pg * p.page_stride + (int64_t)((p0 + row) & page_mask) * width;
-        };
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint16_t* ks = kh + row_of(t * 16 + col) + quad * 8;
-#pragma unroll
-          for (int s = 0; s < R::kSteps; ++s)
-            kn[t][s] = *reinterpret_cast<const uint4*>(ks + s * 32);
-        }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j)
-          vn[j] = *reinterpret_cast<const uint4*>(vh + row_of(j * kPer + lane / kLanes) +
-                                                  lane % kLanes * 8);
-      }
-    };
-
-    int p0 = x.r.from + (x.u0 * kWaves + wave) * kTile;
-    const int p_end = min(x.r.end, x.r.from + x.u1 * kUnit);
-    int page = page_of(entry_at(p0), p0);
-    if (p0 < p_end) load_tile(p0, page);
-    int entry = entry_at(p0 + kUnit);
-    for (; p0 < p_end; p0 += kUnit) {
-      const bool inner = p0 + kTile <= x.r.L && __all(page >= 0);
-      uint32_t there = ~0u;  // positions of the tile that are there at all
-      uint32_t odd = 0;      // rows of V past L that hold infinities or NaN
-      if (!inner) {
-        there = kPages == 1 ? (page >= 0 ? ~0u : 0u) : (uint32_t)__ballot(page >= 0);
-        if (x.r.end - p0 < kTile) there &= (1u << (x.r.end - p0)) - 1;
-        const int ctx = x.r.L - p0;
-        const uint32_t own = ctx <= 0 ? ~0u : ctx >= 32 ? 0u : ~((1u << ctx) - 1);
-        const int row0 = here(lane / kLanes);
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-          const int row = j * kPer + row0;
-          const uint4 was = vn[j];
-          const bool gone = !(there >> row & 1), past = own >> row & 1;
-          const uint4 y = make_uint4(odd_part<T>(was.x, false), odd_part<T>(was.y, false),
-                                     odd_part<T>(was.z, false), odd_part<T>(was.w, false));
-          const bool bad = !gone && past &&
-                           (y.x != was.x || y.y != was.y || y.z != was.z || y.w != was.w);
-          const uint32_t m = gone ? 0u : ~0u;
-          vn[j] = make_uint4(m & (past ? y.x : was.x), m & (past ? y.y : was.y),
-                             m & (past ? y.z : was.z), m & (past ? y.w : was.w));
-          const uint64_t any = __ballot(bad);
-#pragma unroll
-          for (int i = 0; i < kPer; ++i)
-            if (any >> (i * kLanes) & ((2ull << (kLanes - 1)) - 1)) odd |= 1u << (j * kPer + i);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        *reinterpret_cast<uint4*>(vt + (j * kPer + lane / kLanes) * R::kPitch +
-                                  lane % kLanes * 8) = vn[j];
-
-      f32x4 s[kQ][2];
-#pragma unroll
-      for (int st = 0; st < R::kSteps; ++st)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int c = 0; c < kQ; ++c)
-            s[c][t] = mfma<T>(kn[t][st], rows.q[c][st], st ? s[c][t] : f32x4{0, 0, 0, 0});
-
-      // The next loads take the place of this tile's operands: not before.
-      __builtin_amdgcn_sched_barrier(0);
-      const int page_now = page;
-      if (p0 + kUnit < p_end) {
-        page = page_of(entry, p0 + kUnit);
-        load_tile(p0 + kUnit, page);
-        entry = entry_at(p0 + 2 * kUnit);
-      }
-
-      __builtin_amdgcn_sched_barrier(0);
-      uint32_t see[kQ];
-      if (!inner) {
-#pragma unroll
-        for (int c = 0; c < kQ; ++c) see[c] = rows.sees(p, mask, x, c, p0, there);
-        R::hide(s, see, 0);
-      }
-      uint4 pr[1][kQ];
-      rows.weigh(s, p.c, pr);
-      const uint16_t* const vr = vt + (quad * 4 + col / 4) * R::kPitch + (col & 3) * 4;
-      rows.add([&](int h, int d) { return vr + h * 16 * R::kPitch + d * 16; }, pr[0], vh);
-      while (odd) {
-        const int row = __ffs(odd) - 1;
-        odd &= odd - 1;
-        const int pg = kPages == 1 ? page_now : __shfl(page_now, row);
-        rows.add_odd(vh + pg * p.page_stride + (int64_t)((p0 + row) & page_mask) * width, row,
-                     pr[0], see);
-      }
-    }
-
-    // The waves' parts joined, 16 rows at a time through the V tiles' place.
-#pragma unroll
-    for (int c = 0; c < kQ; ++c) {
-      rows.sum[c] = sum4(rows.sum[c]);
-      if (quad == 0) ml[wave * kRows + c * 16 + col] = make_float2(rows.m[c], rows.sum[c]);
-    }
-    __syncthreads();
-    const int64_t slot = 2 * (int64_t)run.me + (at == run.begin ? 0 : 1);
-#pragma unroll
-    for (int c = 0; c < kQ; ++c) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kRows + c * 16 + col].x);
-      const float a = grow(rows.m[c], top);
-      float* const mine = reinterpret_cast<float*>(vt);
-      const int hcol = here(col), hquad = here(quad);
-#pragma unroll
-      for (int d = 0; d < R::kCols; ++d)
-        *reinterpret_cast<f32x4*>(mine + hcol * D + (((d * 4 + hquad) ^ (hcol & 7)) * 4)) =
-            rows.o[c][d] * a;
-      __syncthreads();
-      for (int i = here(threadIdx.x); i < 16 * D / 4; i += kBlock) {
-        const int row = i / (D / 4), ch = i % (D / 4);
-        const int line = x.rt * kRows + c * 16 + row;
-        if (line >= x.r.n * p.G) continue;
-        f32x4 y = f32x4{0, 0, 0, 0};
-        float peak = -INFINITY, whole = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          y += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem) +
-                                               w * (kTile * R::kPitch / 2) + row * D +
-                                               ((ch ^ (row & 7)) * 4));
-          peak = fmaxf(peak, ml[w * kRows + c * 16 + row].x);
-        }
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float2 t = ml[w * kRows + c * 16 + row];
-          whole += t.y * grow(t.x, peak);
-        }
-        if (x.whole && (kKind == kAll || (kKind == kTail && x.r.from == 0))) {
-          const float inv = inverse(whole);
-          const int nd = line / p.G;
-          *reinterpret_cast<uint2*>(p.out + (int64_t)(x.r.first + nd) * p.out_stride +
-                                    (int64_t)(x.g * p.G + line - nd * p.G) * D + ch * 4) =
-              make_uint2(T::pack(y[0] * inv, y[1] * inv), T::pack(y[2] * inv, y[3] * inv));
-        } else {
-          float* to = p.part + (slot * kRows + c * 16 + row) * D;
-          float2* to_ml = p.part_ml + slot * kRows + c * 16 + row;
-          if constexpr (kKind != kAll)
-            if (x.whole) {
-              const int64_t at = whole_row(p, x, line);
-              to = p.whole + at * D;
-              to_ml = p.whole_ml + at;
-            }
-          *reinterpret_cast<f32x4*>(to + ch * 4) = y;
-          if (ch == 0) *to_ml = make_float2(peak, whole);
-        }
-      }
-      __syncthreads();
-    }
-    at += x.u1 - x.u0;
-  }
-}
-
 template <class T, int D, int kQ, int kPages, int kOcc, Kind kKind>
 __global__ __launch_bounds__(kBlock, kOcc) void split_kernel(
     const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
     const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+  using Grid = WholeGrid;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  split_items<T, D, kQ, kPages, kKind>(p, table, off, lengths, mask, smem, whole_grid());
+#include "tg_attn_split.h"
 }
 template <class T, int D, int kQ>
 constexpr size_t split_lds() {
@@ -771,219 +550,14 @@ constexpr size_t split_lds() {
 // banks, as rows of other lengths would do, which these loads cannot write.
 // kEven: a page holds the rows that a wave loads at once, whose address is the
 // wave's then.
-template <class T, int D, int kQ, bool kEven, Kind kKind>
-__device__ __forceinline__ void shared_items(const ParamsOf<kKind>& p,
-                                             const int32_t* __restrict__ table,
-                                             const int32_t* __restrict__ off,
-                                             const int32_t* __restrict__ lengths,
-                                             const uint64_t* __restrict__ mask, uint16_t* tiles,
-                                             int* pre, Blocks at_work) {
-  using R = Rows<T, D, kQ>;
-  constexpr int kRows = 16 * kQ * kWaves, kUnit = 2 * kTile;
-  constexpr int kLanes = D / 8;            // lanes per row
-  constexpr int kHave = kWave / kLanes;    // rows per load of a wave
-  constexpr int kLoads = kUnit / (kHave * kWaves);
-  constexpr int kTileElems = kUnit * D;
-  // tiles: [buffer][K, V][kUnit][D]
-  __shared__ int carry[kWaves];
-  __shared__ uint32_t odd_rows[3][2];  // of the tiles, in turn
-  const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
-  const int col = lane & 15, quad = lane >> 4;
-  auto turn_of = [](int row) { return (D == 64 ? row >> 1 & 3 : row & 7) * 2; };
-
-  Dealer<kRows, kUnit, kKind> run(p, off, lengths, pre, at_work);
-  Piece x = run.first(carry);
-  if (run.begin >= run.stop) {
-    run.leave_none();
-    return;
-  }
-  const int width = p.Hkv * D, page_mask = (1 << p.page_shift) - 1;
-  // The lane's row and chunk in a wave's load (load j: rows j * kHave * kWaves
-  // on; a multiple of 8 rows, so that the chunk is the same in all of them).
-  const int my_row = wave * kHave + lane / kLanes;
-  const int my_chunk = lane % kLanes ^ turn_of(my_row);
-  const uint32_t my_at = (lane / kLanes * width + my_chunk * 8) * 2;
-  // Where the lane reads K (first step) and V (first columns) of a tile.
-  const int k_chunk = quad ^ turn_of(col), v_row = quad * 4 + col / 4;
-  const int v_chunk = (col & 3) / 2 ^ turn_of(v_row);
-  for (int at = run.begin; at < run.stop;) {
-    if (at != run.begin) x = run.at(at);
-    run.leave(x, at);
-    const int32_t* __restrict__ pages = table + (int64_t)x.r.table * p.max_pages;
-    const uint16_t* const kh = p.k + (int64_t)x.g * D;
-    const uint16_t* const vh = p.v + (int64_t)x.g * D;
-    const int row0 = x.rt * kRows + wave * 16 * kQ;
-    const bool busy = row0 < x.r.n * p.G;  // the wave has rows of its own
-    R rows;
-    rows.start(p, x, row0);
-
-    // The table's entry for position p0 + lane and the page that it is, as above.
-    auto entry_at = [&](int p0) -> int {
-      return pages[min(p0 + lane, x.r.end - 1) >> p.page_shift];
-    };
-    auto page_of = [&](int entry, int p0) -> int {
-      return p0 + lane < x.r.end && entry >= 0 && entry < p.n_pages ? entry : -1;
-    };
-    // Starts the loads of the tile at p0 into buffer `buf`; positions without
-    // a page read page 0.
-    auto load_tile = [&](int p0, int page, int buf) {
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = (j * kWaves + wave) * kHave;  // the wave's first
-        lds_u16* const to = (lds_u16*)(tiles + buf * 2 * kTileElems + row * D);
-        if (kEven) {
-          const int64_t from =
-              (int64_t)max(__builtin_amdgcn_readlane(page, row), 0) * p.page_stride +
-              (int64_t)((p0 + row) & page_mask) * width;
-          load_lds16(make_rsrc(kh + from, kHave * width * 2), to, my_at, 0);
-          load_lds16(make_rsrc(vh + from, kHave * width * 2), to + kTileElems, my_at, 0);
-        } else {
-          const int mine = row + lane / kLanes, pg = __shfl(page, mine);
-          const int64_t from = (pg < 0 ? 0 : pg * p.page_stride +
-                                (int64_t)((p0 + mine) & page_mask) * width) + my_chunk * 8;
-          load_lds(kh + from, to);
-          load_lds(vh + from, to + kTileElems);
-        }
-      }
-    };
-    // Waits for the wave's own loads of the tile at p0 and mends its rows of V:
-    // those that are not there become 0, infinities and NaN past L too, noted.
-    auto finish_tile = [&](int p0, int page, int buf, int turn) {
-      TG_WAIT_VM(0);
-      asm volatile("" ::: "memory");
-      if (p0 + kUnit <= x.r.L && __all(page >= 0)) return;
-      const unsigned long long there = __ballot(page >= 0);
-#pragma unroll 1
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = (j * kWaves + wave) * kHave + lane / kLanes;
-        const bool gone = !(there >> row & 1), own = p0 + row >= x.r.L;
-        u32x4* const place = reinterpret_cast<u32x4*>(
-            tiles + (buf * 2 + 1) * kTileElems + (j * kWaves + wave) * kHave * D + lane * 8);
-        u32x4 y = *place;
-        uint32_t bad = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t odd = own ? odd_part<T>(y[i], true) : 0u;
-          y[i] = gone ? 0u : y[i] ^ odd;
-          bad |= odd;
-        }
-        if (bad && !gone) atomicOr(&odd_rows[turn][row / 32], 1u << (row % 32));
-        *place = y;
-      }
-    };
-
-    int p0 = x.r.from + x.u0 * kUnit, buf = 0, turn = 0;
-    const int p_end = x.r.from + x.u1 * kUnit;
-    int page = page_of(entry_at(p0), p0), entry = entry_at(p0 + kUnit);
-    __syncthreads();  // the last piece's reads are over
-    if (threadIdx.x < 6) odd_rows[threadIdx.x / 2][threadIdx.x % 2] = 0;
-    load_tile(p0, page, 0);
-    __syncthreads();
-    finish_tile(p0, page, 0, 0);
-    __syncthreads();
-    for (; p0 < p_end; p0 += kUnit, buf ^= 1) {
-      const bool more = p0 + kUnit < p_end;
-      const int page_now = page;
-      const uint16_t* const kt = tiles + buf * 2 * kTileElems;
-      f32x4 s[kQ][4];
-      if (busy) rows.scores(kt + col * D, k_chunk, s, kh);
-      if (more) {
-        page = page_of(entry, p0 + kUnit);
-        load_tile(p0 + kUnit, page, buf ^ 1);
-        entry = entry_at(p0 + 2 * kUnit);
-      }
-      const bool inner = p0 + kUnit <= x.r.L && __all(page_now >= 0);
-      if (busy) {
-        const unsigned long long there64 = inner ? ~0ull : __ballot(page_now >= 0);
-        uint32_t see[2][kQ];
-        if (!inner) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint32_t there = (uint32_t)(there64 >> (half * 32));
-#pragma unroll
-            for (int c = 0; c < kQ; ++c)
-              see[half][c] = rows.sees(p, mask, x, c, p0 + half * kTile, there);
-            R::hide(s, see[half], half);
-          }
-        }
-        uint4 pr[2][kQ];
-        rows.weigh(s, p.c, pr);
-        const uint16_t* const vr = kt + kTileElems + v_row * D + (col & 1) * 4;
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-          rows.add([&](int h, int d) {
-            return vr + (half * kTile + h * 16) * D + (v_chunk ^ (d * 2)) * 8;
-          }, pr[half], vh);
-        if (!inner) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t odd = odd_rows[turn][half];
-            while (odd) {
-              const int row = __ffs(odd) - 1;
-              odd &= odd - 1;
-              const int pg = __shfl(page_now, half * kTile + row);
-              rows.add_odd(vh + pg * p.page_stride +
-                               (int64_t)((p0 + half * kTile + row) & page_mask) * width,
-                           row, pr[half], see[half]);
-            }
-          }
-        }
-      }
-      // One tile's notes are read, the next one's written, and those of the
-      // one after it (read before the last barrier) cleared.
-      const int next = turn == 2 ? 0 : turn + 1;
-      if (threadIdx.x < 2) odd_rows[next == 2 ? 0 : next + 1][threadIdx.x] = 0;
-      if (more) finish_tile(p0 + kUnit, page, buf ^ 1, next);
-      turn = next;
-      __syncthreads();
-    }
-
-    const int64_t slot = 2 * (int64_t)run.me + (at == run.begin ? 0 : 1);
-    if (busy) {
-#pragma unroll
-      for (int c = 0; c < kQ; ++c) {
-        const float whole = sum4(rows.sum[c]);
-        const int line = row0 + c * 16 + col;
-        if (line < x.r.n * p.G) {
-          if (x.whole && (kKind == kAll || (kKind == kTail && x.r.from == 0))) {
-            const float inv = inverse(whole);
-            uint16_t* const to = p.out + (int64_t)(x.r.first + rows.node[c]) * p.out_stride +
-                                 (int64_t)(x.g * p.G + line - rows.node[c] * p.G) * D + quad * 4;
-#pragma unroll
-            for (int d = 0; d < R::kCols; ++d) {
-              const f32x4 y = rows.o[c][d] * inv;
-              *reinterpret_cast<uint2*>(to + d * 16) =
-                  make_uint2(T::pack(y[0], y[1]), T::pack(y[2], y[3]));
-            }
-          } else {
-            const int64_t line_at = slot * kRows + wave * 16 * kQ + c * 16 + col;
-            float* to = p.part + line_at * D;
-            float2* to_ml = p.part_ml + line_at;
-            if constexpr (kKind != kAll)
-              if (x.whole) {
-                const int64_t at = whole_row(p, x, line);
-                to = p.whole + at * D;
-                to_ml = p.whole_ml + at;
-              }
-#pragma unroll
-            for (int d = 0; d < R::kCols; ++d)
-              *reinterpret_cast<f32x4*>(to + d * 16 + quad * 4) = rows.o[c][d];
-            if (quad == 0) *to_ml = make_float2(rows.m[c], whole);
-          }
-        }
-      }
-    }
-    at += x.u1 - x.u0;
-  }
-}
-
 template <class T, int D, int kQ, bool kEven, int kOcc, Kind kKind>
 __global__ __launch_bounds__(kBlock, kOcc) void shared_kernel(
     const ParamsOf<kKind> p, const int32_t* __restrict__ table, const int32_t* __restrict__ off,
     const int32_t* __restrict__ lengths, const uint64_t* __restrict__ mask) {
+  using Grid = WholeGrid;
   __shared__ __attribute__((aligned(16))) uint16_t tiles[8 * kTile * D];
   extern __shared__ __attribute__((aligned(16))) int pre[];
-  shared_items<T, D, kQ, kEven, kKind>(p, table, off, lengths, mask, tiles, pre, whole_grid());
+#include "tg_attn_shared.h"
 }
 
 // Which kernel: the rows of one KV head that requests have (at most, or as a
