@@ -32,32 +32,6 @@ struct PlanParams {
   Group* group;                    // [groups]
 };
 
-// pre[i + 1] = units(0) + ... + units(i), pre[0] = 0.
-template <class Units>
-__device__ __forceinline__ void sum_units(int n, int32_t* pre, int* carry, Units units) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int base = 0;
-  for (int i0 = 0; i0 < n; i0 += kPlanBlock) {
-    const int i = i0 + threadIdx.x;
-    int x = i < n ? units(i) : 0;
-    for (int m = 1; m < kWave; m *= 2) {
-      const int o = __shfl_up(x, m);
-      if (lane >= m) x = add_units(x, o);
-    }
-    __syncthreads();
-    if (lane == kWave - 1) carry[wave] = x;
-    __syncthreads();
-    int front = base;
-    for (int w = 0; w < kPlanWaves; ++w) {
-      if (w < wave) front = add_units(front, carry[w]);
-      base = add_units(base, carry[w]);
-    }
-    if (i < n) pre[i + 1] = add_units(front, x);
-  }
-  if (threadIdx.x == 0) pre[0] = 0;
-  __syncthreads();
-}
-
 // The last i in [0, n) with a[i] <= x, 0 if there is none.
 __device__ __forceinline__ int last_at(const int* a, int n, int x) {
   int i = 0;
@@ -69,66 +43,110 @@ __device__ __forceinline__ int last_at(const int* a, int n, int x) {
   return i;
 }
 
+// Every thread has the requests and the groups tid, tid + kPlanBlock and so on; what
+// it reads of them is read at once.
 __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
-  __shared__ int starts[kMaxRequests + 1];  // of groups, then of requests' rows
+  constexpr int kEach = kMaxRequests / kPlanBlock;
+  __shared__ int starts[kMaxRequests + 1];  // of groups: a request
+  __shared__ int rows[kMaxRequests + 1];    // of requests: a row
   __shared__ int least[kMaxRequests];       // of a group: its shared positions
   __shared__ int members[kMaxRequests];     // with rows
-  __shared__ int carry[kPlanWaves];
-  const int tid = threadIdx.x;
+  __shared__ int carry[2][kPlanWaves];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int first[kEach], next[kEach], length[kEach], group[kEach];
   // Offsets that do not ascend from 0 to B stay inside all arrays.
-  for (int g = tid; g <= p.groups; g += kPlanBlock)
-    starts[g] = max(0, min(p.group_off[g], p.B));
-  for (int g = tid; g < p.groups; g += kPlanBlock) {
-    least[g] = max(0, min(p.shared[g], p.cap));
-    members[g] = 0;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = k * kPlanBlock + tid;
+    if (i < p.B) {
+      first[k] = p.off[i];
+      next[k] = p.off[i + 1];
+      length[k] = p.lengths[i];
+    }
+    if (i < p.groups) {
+      starts[i] = max(0, min(p.group_off[i], p.B));
+      least[i] = max(0, min(p.shared[i], p.cap));
+      members[i] = 0;
+    }
+  }
+  if (tid == 0) {
+    rows[p.B] = max(0, min(p.off[p.B], p.T));
+    starts[p.groups] = p.groups ? max(0, min(p.group_off[p.groups], p.B)) : 0;
   }
   __syncthreads();
-  for (int b = tid; b < p.B; b += kPlanBlock) {
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int b = k * kPlanBlock + tid;
+    if (b >= p.B) break;
     int g = p.groups ? last_at(starts, p.groups, b) : -1;
     if (g >= 0 && (b < starts[g] || b >= starts[g + 1])) g = -1;
-    p.group_of[b] = g;
-    int first, n;
-    request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
-    if (g >= 0 && n > 0) {
-      atomicMin(&least[g], max(0, p.lengths[b]));
+    p.group_of[b] = group[k] = g;
+    first[k] = max(0, min(first[k], p.T));
+    next[k] = max(0, min(next[k], p.T));
+    rows[b] = first[k];
+    if (g >= 0 && next[k] > first[k]) {
+      atomicMin(&least[g], max(0, length[k]));
       atomicAdd(&members[g], 1);
     }
   }
   __syncthreads();
   // One request alone shares nothing.
-  for (int g = tid; g < p.groups; g += kPlanBlock) {
+  int units[2][kEach] = {};  // of groups, of requests
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int g = k * kPlanBlock + tid;
+    if (g >= p.groups) break;
     const int shared = members[g] > 1 ? least[g] / kWholeUnits * kWholeUnits : 0;
     least[g] = shared;
     Group x;
     const int b0 = starts[g], b1 = max(b0, starts[g + 1]);
-    x.first = max(0, min(p.off[b0], p.T));
-    x.n = shared ? max(x.first, min(p.off[b1], p.T)) - x.first : 0;
+    x.first = rows[b0];
+    x.n = shared ? max(x.first, rows[b1]) - x.first : 0;
     x.positions = shared;
     x.request = min(b0, p.B - 1);
     p.group[g] = x;
+    units[0][k] = (x.positions + p.prefix_unit - 1) / p.prefix_unit *
+                  ((x.n * p.G + p.prefix_rows - 1) / p.prefix_rows) * p.Hkv;
   }
   __syncthreads();
-  for (int b = tid; b < p.B; b += kPlanBlock) {
-    const int g = p.group_of[b];
-    p.from[b] = g >= 0 ? least[g] : 0;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int b = k * kPlanBlock + tid;
+    if (b >= p.B) break;
+    const int from = group[k] >= 0 ? least[group[k]] : 0;
+    p.from[b] = from;
+    const int n = max(0, min(next[k] - first[k], p.max_nodes));
+    const int L = max(0, min(length[k], p.cap)), end = min(L + n, p.cap);
+    units[1][k] = (end - from + p.tail_unit - 1) / p.tail_unit *
+                  ((n * p.G + p.tail_rows - 1) / p.tail_rows) * p.Hkv;
   }
-  sum_units(p.groups, p.pre_prefix, carry, [&](int g) {
-    const Group x = p.group[g];
-    return (x.positions + p.prefix_unit - 1) / p.prefix_unit *
-           ((x.n * p.G + p.prefix_rows - 1) / p.prefix_rows) * p.Hkv;
-  });
-  sum_units(p.B, p.pre_tail, carry, [&](int b) {
-    int first, n;
-    request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
-    const int L = max(0, min(p.lengths[b], p.cap)), end = min(L + n, p.cap);
-    return (end - p.from[b] + p.tail_unit - 1) / p.tail_unit *
-           ((n * p.G + p.tail_rows - 1) / p.tail_rows) * p.Hkv;
-  });
-  for (int b = tid; b <= p.B; b += kPlanBlock) starts[b] = max(0, min(p.off[b], p.T));
-  __syncthreads();
+  // Both running sums.
+  int base[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    if (k * kPlanBlock >= max(p.B, p.groups)) break;
+    int x[2] = {units[0][k], units[1][k]};
+    for (int m = 1; m < kWave; m *= 2) {
+      const int o[2] = {__shfl_up(x[0], m), __shfl_up(x[1], m)};
+      if (lane >= m) x[0] = add_units(x[0], o[0]), x[1] = add_units(x[1], o[1]);
+    }
+    if (k) __syncthreads();
+    if (lane == kWave - 1) carry[0][wave] = x[0], carry[1][wave] = x[1];
+    __syncthreads();
+    const int i = k * kPlanBlock + tid;
+    for (int j = 0; j < 2; ++j) {
+      int front = base[j];
+      for (int w = 0; w < kPlanWaves; ++w) {
+        if (w < wave) front = add_units(front, carry[j][w]);
+        base[j] = add_units(base[j], carry[j][w]);
+      }
+      if (i < (j ? p.B : p.groups)) (j ? p.pre_tail : p.pre_prefix)[i + 1] = add_units(front, x[j]);
+    }
+  }
+  if (tid == 0) p.pre_prefix[0] = p.pre_tail[0] = 0;
   for (int t = tid; t < p.T; t += kPlanBlock) {
-    const int b = last_at(starts, p.B, t);
-    p.request_of_row[t] = t >= starts[b] && t < min(starts[b + 1], starts[b] + p.max_nodes) ? b : -1;
+    const int b = last_at(rows, p.B, t);
+    p.request_of_row[t] = t >= rows[b] && t < min(rows[b + 1], rows[b] + p.max_nodes) ? b : -1;
   }
 }
 
@@ -164,15 +182,15 @@ struct Joined {
   }
 };
 
-// Adds the parts of a row: line `line` of head g of item group `b`, whose items are
-// `tiles` times `units` units; `row`: its place among whole items' rows.
+// Adds the parts of a row: line `line` of head g of the items from unit `pre` of
+// `total` on, `tiles` times `units` units a head; `row`: its place among whole items' rows.
 template <int D>
-__device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, int b, int g, int line,
+__device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, int pre, int g, int line,
                                           int units, int tiles, int64_t row, int ch) {
   if (units <= 0) return;
   constexpr int kU = 8;
   const int share = max(1, (total + s.blocks - 1) / s.blocks);
-  const int start = s.pre[b] + (g * tiles + line / s.rows) * units;
+  const int start = pre + (g * tiles + line / s.rows) * units;
   const int k0 = start / share, parts = (start + units - 1) / share - k0 + 1;
   if (parts == 1) {
     j.add(*reinterpret_cast<const f32x4*>(s.whole + row * D + ch * 4), s.whole_ml[row]);
@@ -205,29 +223,32 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) 
   const int head = (blockIdx.y * kWaves + wave) * kAt + lane / kLine;
   if (b < 0 || head >= Hq) return;
   const int g = head / p.G, jj = head - g * p.G;
-  const int from = p.from[b];
+  const int from = p.from[b], gr = p.group_of[b];
   int first, n;
   request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
   const int L = max(0, min(p.lengths[b], p.cap)), end = min(L + n, p.cap);
+  const int total = p.tail.pre[p.B], pre = p.tail.pre[b];
   const int units = (end - from + p.tail.unit - 1) / p.tail.unit;
   const int tiles = (n * p.G + p.tail.rows - 1) / p.tail.rows;
-  const int line = (t - first) * p.G + jj, total = p.tail.pre[p.B];
+  const int line = (t - first) * p.G + jj;
   const int64_t row = (int64_t)t * Hq + head;
-  if (from == 0) {  // one block's rows are there already
+  Group x = {};
+  int prefix_total = 0, prefix_pre = 0;
+  if (from > 0) {
+    x = p.group[gr];
+    prefix_total = p.prefix.pre[p.groups];
+    prefix_pre = p.prefix.pre[gr];
+  } else {  // one block's rows are there already
     const int share = max(1, (total + p.tail.blocks - 1) / p.tail.blocks);
-    const int start = p.tail.pre[b] + (g * tiles + line / p.tail.rows) * units;
+    const int start = pre + (g * tiles + line / p.tail.rows) * units;
     if (start / share == (start + units - 1) / share) return;
   }
   Joined j;
-  add_parts<D>(j, p.tail, total, b, g, line, units, tiles, row, ch);
-  if (from > 0) {
-    const int gr = p.group_of[b];
-    const Group x = p.group[gr];
-    if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
-      add_parts<D>(j, p.prefix, p.prefix.pre[p.groups], gr, g, (t - x.first) * p.G + jj,
-                   (x.positions + p.prefix.unit - 1) / p.prefix.unit,
-                   (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch);
-  }
+  add_parts<D>(j, p.tail, total, pre, g, line, units, tiles, row, ch);
+  if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
+    add_parts<D>(j, p.prefix, prefix_total, prefix_pre, g, (t - x.first) * p.G + jj,
+                 (x.positions + p.prefix.unit - 1) / p.prefix.unit,
+                 (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch);
   const float inv = inverse(j.sum);
   *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + ch * 4) =
       make_uint2(T::pack(j.o[0] * inv, j.o[1] * inv), T::pack(j.o[2] * inv, j.o[3] * inv));
