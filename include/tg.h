@@ -530,12 +530,12 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
  * rows instead of once per request.
  *
  * Group g is requests group_offsets[g] .. group_offsets[g+1]-1 (device array
- * [n_groups+1], non-decreasing, from 0 to B). The first shared[g] positions of all
- * of them lie in the same pages: they are read through the table row of the
- * group's first request. shared[g] may be anything from 0 on; what counts is the
- * largest multiple of 128 that neither it nor the length of any request of the
- * group with rows exceeds (0 for one request alone), and requests outside all
- * groups share nothing. Results are tg_tree_attention's up to the last bits.
+ * [n_groups+1], non-decreasing, from 0 to B). The first shared[g] positions of its
+ * requests that have rows lie in the same pages, which are read through the table
+ * row of the first of these (what the others' tables and lengths hold does not
+ * count). shared[g] may be anything from 0 on; what counts is the largest multiple
+ * of 128 that neither it nor the length of any such request exceeds (0 for one
+ * alone), and requests outside all groups share nothing. Results are tg_tree_attention's up to the last bits.
  * Groups are dealt out by the mean rows of a group, T / n_groups; any are right.
  * The limit is, besides tg_tree_attention's,
  *   Hkv * (T * G' + n_groups) * max_pages * page_size / 64 < 2^30.

@@ -50,7 +50,8 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   __shared__ int starts[kMaxRequests + 1];  // of groups: a request
   __shared__ int rows[kMaxRequests + 1];    // of requests: a row
   __shared__ int least[kMaxRequests];       // of a group: its shared positions
-  __shared__ int members[kMaxRequests];     // with rows
+  __shared__ int member[kMaxRequests];      // the first one with rows
+  __shared__ int last[kMaxRequests];        // and the last
   __shared__ int carry[2][kPlanWaves];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   int first[kEach], next[kEach], length[kEach], group[kEach];
@@ -66,7 +67,8 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
     if (i < p.groups) {
       starts[i] = max(0, min(p.group_off[i], p.B));
       least[i] = max(0, min(p.shared[i], p.cap));
-      members[i] = 0;
+      member[i] = p.B;
+      last[i] = -1;
     }
   }
   if (tid == 0) {
@@ -86,7 +88,8 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
     rows[b] = first[k];
     if (g >= 0 && next[k] > first[k]) {
       atomicMin(&least[g], max(0, length[k]));
-      atomicAdd(&members[g], 1);
+      atomicMin(&member[g], b);
+      atomicMax(&last[g], b);
     }
   }
   __syncthreads();
@@ -96,14 +99,14 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   for (int k = 0; k < kEach; ++k) {
     const int g = k * kPlanBlock + tid;
     if (g >= p.groups) break;
-    const int shared = members[g] > 1 ? least[g] / kWholeUnits * kWholeUnits : 0;
+    const int shared = member[g] < last[g] ? least[g] / kWholeUnits * kWholeUnits : 0;
     least[g] = shared;
     Group x;
     const int b0 = starts[g], b1 = max(b0, starts[g + 1]);
     x.first = rows[b0];
     x.n = shared ? max(x.first, rows[b1]) - x.first : 0;
     x.positions = shared;
-    x.request = min(b0, p.B - 1);
+    x.request = min(member[g], p.B - 1);
     p.group[g] = x;
     units[0][k] = (x.positions + p.prefix_unit - 1) / p.prefix_unit *
                   ((x.n * p.G + p.prefix_rows - 1) / p.prefix_rows) * p.Hkv;

@@ -129,6 +129,18 @@ def test_positions_without_a_page_are_not_there():
     run(x, groups, 4, 64)
 
 
+@pytest.mark.parametrize("length", [400, 0])
+def test_a_request_without_rows_says_nothing_of_the_prefix(length):
+    """A sample that has ended: its pages given back, its length still there or not."""
+    requests, groups = [(400, 0), (420, 1), (0, 0), (410, 2)], [(0, 4, 400)]
+    x = make(requests, groups, 4, 2, 128, BF, 16, 4)
+    cache, table, off, L, q, m = x
+    table[[0, 2]] = -1
+    L[0] = length
+    cache.page_table.copy_(torch.from_numpy(table))
+    run(x, groups, 4, 128)
+
+
 def test_infinities_stay_with_the_rows_that_see_them():
     requests, groups = [(300, 4), (310, 2)], [(0, 2, 288)]
     x = make(requests, groups, 4, 2, 128, BF, 16, 3, fill=float("inf"))
