@@ -284,32 +284,52 @@ struct Weigh {
   }
 };
 
-__device__ __forceinline__ u64 shfl_up64(u64 x, int by) {
-  const uint32_t lo = __shfl_up((uint32_t)x, by), hi = __shfl_up((uint32_t)(x >> 32), by);
+// Scans and reductions over a wave's lanes by DPP (of 64 bits, 12 instructions and 6
+// operations, where shuffles through LDS have six latencies of it in a row: the draw
+// of one row ONEROW us). All lanes take part; `none`: what op leaves as it is.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ u64 dpp64(u64 x, u64 none) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, kCtrl, kRows, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp((int)(none >> 32), (int)(x >> 32), kCtrl,
+                                                            kRows, 0xF, false);
   return (u64)hi << 32 | lo;
 }
-__device__ __forceinline__ u64 shfl_xor64(u64 x, int by) {
-  const uint32_t lo = __shfl_xor((uint32_t)x, by), hi = __shfl_xor((uint32_t)(x >> 32), by);
-  return (u64)hi << 32 | lo;
-}
-__device__ __forceinline__ u64 wave_sum(u64 x) {
-  for (int o = 1; o < kWave; o *= 2) x += shfl_xor64(x, o);
+template <class Op>
+__device__ __forceinline__ u64 wave_scan(u64 x, u64 none, Op op) {
+  x = op(x, dpp64<0x111, 0xF>(x, none));  // row_shr:1
+  x = op(x, dpp64<0x112, 0xF>(x, none));
+  x = op(x, dpp64<0x114, 0xF>(x, none));
+  x = op(x, dpp64<0x118, 0xF>(x, none));
+  x = op(x, dpp64<0x142, 0xA>(x, none));  // row_bcast:15
+  x = op(x, dpp64<0x143, 0xC>(x, none));  // row_bcast:31
   return x;
 }
+template <class Op>
+__device__ __forceinline__ u64 wave_all(u64 x, u64 none, Op op) {
+  x = wave_scan(x, none, op);
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), kWave - 1) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((int)x, kWave - 1);
+}
+struct Add {
+  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return max(a, b); }
+};
+struct Min {
+  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return min(a, b); }
+};
+__device__ __forceinline__ u64 wave_sum(u64 x) { return wave_all(x, 0, Add{}); }
+__device__ __forceinline__ u64 wave_max(u64 x) { return wave_all(x, 0, Max{}); }
+__device__ __forceinline__ u64 wave_min(u64 x) { return wave_all(x, ~0ull, Min{}); }
 
 // Inclusive sums over the block's threads; the whole in *total. lds, lds_n: an
 // entry per wave; n and lds_n may be null.
 template <int kWaves>
 __device__ __forceinline__ void scan(u64* lds, uint32_t* lds_n, u64* x, uint32_t* n, u64* total) {
   const int lane = (int)__lane_id(), wave = threadIdx.x / kWave;
-  for (int m = 1; m < kWave; m *= 2) {
-    const u64 o = shfl_up64(*x, m);
-    const uint32_t q = n ? __shfl_up(*n, m) : 0;
-    if (lane >= m) {
-      *x += o;
-      if (n) *n += q;
-    }
-  }
+  *x = wave_scan(*x, 0, Add{});
+  if (n) *n = (uint32_t)wave_scan(*n, 0, Add{});
   __syncthreads();
   if (lane == kWave - 1) {
     lds[wave] = *x;
@@ -363,7 +383,7 @@ __global__ __launch_bounds__(kPartBlock) void part_kernel(const uint8_t* __restr
     }
     best = key_of(most, first);
   }
-  for (int o = 1; o < kWave; o *= 2) best = max(best, shfl_xor64(best, o));
+  best = wave_max(best);
   if (__lane_id() == 0) tops[wave] = best;
   __syncthreads();
 #pragma unroll
@@ -430,7 +450,7 @@ __device__ __forceinline__ void find_cut(const Params& p, const Filters& f, int 
   const u64* const bests = p.sp.best + (int64_t)t * p.parts;
   u64 best = 0;
   for (int i = tid; i < p.parts; i += kThreads) best = max(best, bests[i]);
-  for (int o = 1; o < kWave; o *= 2) best = max(best, shfl_xor64(best, o));
+  best = wave_max(best);
   if (__lane_id() == 0) sh.tops[tid / kWave] = best;
   __syncthreads();
   for (int i = 0; i < kWaves; ++i) best = max(best, sh.tops[i]);
@@ -766,8 +786,7 @@ __device__ __forceinline__ void settle_picked(DrawShared& sh, const Weigh& weigh
     }
   }
   const bool stays = w && nb < most && mb < mass;
-  u64 least = stays ? key : ~0ull;
-  for (int o = 1; o < kWave; o *= 2) least = min(least, shfl_xor64(least, o));
+  u64 least = wave_min(stays ? key : ~0ull);
   if (least == ~0ull) least = cut;  // the border is among tokens without weight
   const u64 sum = wave_sum(stays ? w : 0);
   if (lane == 0) {
@@ -806,10 +825,8 @@ __device__ __forceinline__ u64 settle(DrawShared& sh, const Border<T>& border, u
       lo = min(lo, o);
       hi = max(hi, o);
     }
-    for (int o = 1; o < kWave; o *= 2) {
-      lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
-      hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
-    }
+    lo = (uint32_t)wave_min(lo);
+    hi = (uint32_t)wave_max(hi);
     if (__lane_id() == 0) {
       atomicMin(&sh.lo32, lo);
       atomicMax(&sh.hi32, hi);
@@ -901,7 +918,7 @@ __global__ __launch_bounds__(kDrawBlock) void draw_kernel(const uint8_t* __restr
     __syncthreads();
   } else {
     for (int i = tid; i < p.parts; i += kDrawBlock) best = max(best, bests[i]);
-    for (int o = 1; o < kWave; o *= 2) best = max(best, shfl_xor64(best, o));
+    best = wave_max(best);
     if (__lane_id() == 0) sh.scan[tid / kWave] = best;
     __syncthreads();
     for (int i = 0; i < kDrawWaves; ++i) best = max(best, sh.scan[i]);
