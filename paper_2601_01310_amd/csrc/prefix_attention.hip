@@ -12,7 +12,7 @@
 //           length, whole units of 128 positions), and the units of work before
 //           each group and request;
 //   prefix, tail;
-//   join    a wave takes a few heads of a row, its parts in one loop.
+//   join    a block takes one to four heads of a row, a wave every fourth part.
 #include "tg_attn.h"
 
 namespace tg {
@@ -187,25 +187,26 @@ struct Joined {
 
 // Adds the parts of a row: line `line` of head g of the items from unit `pre` of
 // `total` on, `tiles` times `units` units a head; `row`: its place among whole items' rows.
+// Every wave adds every fourth one.
 template <int D>
 __device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, int pre, int g, int line,
-                                          int units, int tiles, int64_t row, int ch) {
+                                          int units, int tiles, int64_t row, int ch, int wave) {
   if (units <= 0) return;
-  constexpr int kU = 8;
+  constexpr int kU = 4;
   const int share = max(1, (total + s.blocks - 1) / s.blocks);
   const int start = pre + (g * tiles + line / s.rows) * units;
   const int k0 = start / share, parts = (start + units - 1) / share - k0 + 1;
   if (parts == 1) {
-    j.add(*reinterpret_cast<const f32x4*>(s.whole + row * D + ch * 4), s.whole_ml[row]);
+    if (wave == 0) j.add(*reinterpret_cast<const f32x4*>(s.whole + row * D + ch * 4), s.whole_ml[row]);
     return;
   }
   const int slot = start == k0 * share ? 0 : 1, at = line % s.rows;
-  for (int k = 0; k < parts; k += kU) {
+  for (int k = wave; k < parts; k += kU * kWaves) {
     f32x4 x[kU];
     float2 ml[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const int i = min(k + u, parts - 1);
+      const int i = min(k + u * kWaves, parts - 1);
       const int block = min(k0 + i, s.blocks - 1);
       const int64_t place = (2 * (int64_t)block + (i == 0 ? slot : 0)) * s.rows + at;
       x[u] = *reinterpret_cast<const f32x4*>(s.part + place * D + ch * 4);
@@ -213,7 +214,7 @@ __device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, 
     }
 #pragma unroll
     for (int u = 0; u < kU; ++u)
-      if (k + u < parts) j.add(x[u], ml[u]);
+      if (k + u * kWaves < parts) j.add(x[u], ml[u]);
   }
 }
 
@@ -223,8 +224,10 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) 
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int t = blockIdx.x, Hq = p.Hkv * p.G, ch = lane % kLine;
   const int b = p.request_of_row[t];
-  const int head = (blockIdx.y * kWaves + wave) * kAt + lane / kLine;
-  if (b < 0 || head >= Hq) return;
+  __shared__ f32x4 os[kWaves][kWave];
+  __shared__ float2 mls[kWaves][kWave];
+  if (b < 0) return;
+  const int head0 = blockIdx.y * kAt + lane / kLine, head = min(head0, Hq - 1);
   const int g = head / p.G, jj = head - g * p.G;
   const int from = p.from[b], gr = p.group_of[b];
   int first, n;
@@ -235,23 +238,26 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) 
   const int tiles = (n * p.G + p.tail.rows - 1) / p.tail.rows;
   const int line = (t - first) * p.G + jj;
   const int64_t row = (int64_t)t * Hq + head;
-  Group x = {};
-  int prefix_total = 0, prefix_pre = 0;
+  Joined j;
+  bool there = false;  // one block's rows are in the output already
   if (from > 0) {
-    x = p.group[gr];
-    prefix_total = p.prefix.pre[p.groups];
-    prefix_pre = p.prefix.pre[gr];
-  } else {  // one block's rows are there already
+    const Group x = p.group[gr];
+    if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
+      add_parts<D>(j, p.prefix, p.prefix.pre[p.groups], p.prefix.pre[gr], g,
+                   (t - x.first) * p.G + jj, (x.positions + p.prefix.unit - 1) / p.prefix.unit,
+                   (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch, wave);
+  } else {
     const int share = max(1, (total + p.tail.blocks - 1) / p.tail.blocks);
     const int start = pre + (g * tiles + line / p.tail.rows) * units;
-    if (start / share == (start + units - 1) / share) return;
+    there = start / share == (start + units - 1) / share;
   }
-  Joined j;
-  add_parts<D>(j, p.tail, total, pre, g, line, units, tiles, row, ch);
-  if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
-    add_parts<D>(j, p.prefix, prefix_total, prefix_pre, g, (t - x.first) * p.G + jj,
-                 (x.positions + p.prefix.unit - 1) / p.prefix.unit,
-                 (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch);
+  if (!there) add_parts<D>(j, p.tail, total, pre, g, line, units, tiles, row, ch, wave);
+  os[wave][lane] = j.o;
+  mls[wave][lane] = make_float2(j.m, j.sum);
+  __syncthreads();
+  if (wave > 0 || there || head0 >= Hq) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) j.add(os[w][lane], mls[w][lane]);
   const float inv = inverse(j.sum);
   *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + ch * 4) =
       make_uint2(T::pack(j.o[0] * inv, j.o[1] * inv), T::pack(j.o[2] * inv, j.o[3] * inv));
@@ -456,7 +462,7 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
   j.max_nodes = x.max_nodes;
   j.B = c.B;
   j.groups = a->n_groups;
-  constexpr int kHeads = kWaves * (kWave / (D / 4));  // per block
+  constexpr int kHeads = kWave / (D / 4);  // per block
   hipLaunchKernelGGL((join_parts_kernel<T, D>), dim3(x.T, (x.Hq + kHeads - 1) / kHeads), dim3(kBlock),
                      0, s, j);
   return hipGetLastError();

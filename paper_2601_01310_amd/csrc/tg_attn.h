@@ -228,9 +228,18 @@ struct Dealer {
 
   __device__ __forceinline__ void runs(int total) {
     const int blocks = Grid::blocks();
-    // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
-    me = (Grid::block() % Grid::kXcds) * (blocks / (int)Grid::kXcds) + Grid::block() / Grid::kXcds;
     share = max(1, (total + blocks - 1) / blocks);
+    // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
+    int each = blocks / (int)Grid::kXcds;
+    if constexpr (kKind != kAll) {  // few runs are spread over all XCDs
+      const int used = (total + share - 1) / share;
+      each = (used + (int)Grid::kXcds - 1) / (int)Grid::kXcds;
+      if ((int)(Grid::block() / Grid::kXcds) >= each) {
+        begin = stop = 0;
+        return;
+      }
+    }
+    me = (Grid::block() % Grid::kXcds) * each + Grid::block() / Grid::kXcds;
     begin = (int)min((int64_t)total, (int64_t)me * share);
     stop = min(total, begin + share);
   }
