@@ -228,9 +228,10 @@ tg_status tg_ew_forward_timed(const tg_ew_args* a, void* ws, size_t ws_bytes, vo
 tg_status tg_ew_forward_noalloc(const tg_ew_args* a, void* stream);
 
 /*
- * The EW forward for a few tokens (a decode step of few requests), in two
- * kernels that stream the touched slots' weights (three with w_gate): gating, the
- * routing table, the SwiGLU experts and the weighted sum of tg_ew_forward, for
+ * The EW forward for a few tokens (a decode step of few requests): two kernels
+ * that stream the touched slots' weights, with one before them for more than a few
+ * logits of w_gate and one behind for the sums of more tokens. Gating, the routing
+ * table, the SwiGLU experts and the weighted sum of tg_ew_forward, for
  * T <= TG_MAX_FEW tokens with T * k <= TG_MAX_FEW_PAIRS.
  *
  * ids, weights, slots and n_unserved have tg_ew_forward's bits. The experts'
@@ -535,7 +536,9 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
  * row of the first of these (what the others' tables and lengths hold does not
  * count). shared[g] may be anything from 0 on; what counts is the largest multiple
  * of 128 that neither it nor the length of any such request exceeds (0 for one
- * alone), and requests outside all groups share nothing. Results are tg_tree_attention's up to the last bits.
+ * alone), and requests outside all groups share nothing. Results are
+ * tg_tree_attention's up to the last bits; a call without groups, or whose page
+ * tables hold so few positions that sharing could save little, is that call.
  * Groups are dealt out by the mean rows of a group, T / n_groups; any are right.
  * The limit is, besides tg_tree_attention's,
  *   Hkv * (T * G' + n_groups) * max_pages * page_size / 64 < 2^30.

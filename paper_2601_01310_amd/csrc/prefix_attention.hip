@@ -479,7 +479,19 @@ hipError_t launch_type(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
 
 }  // namespace
 
+// Whether reading a prefix once could save so little that the plan and the longer
+// join cost more, by what the page tables can hold: heads 32 / 8 of 128, bf16, one
+// token each behind 200 tokens of their own, tree attention and this one (us): 4
+// requests behind 1000 shared positions 12.6 and 17.2, 8 behind 512 11.9 and 17.5; 4
+// behind 2048 20.0 and 17.3, 8 behind 2048 21.5 and 18.9.
+static bool little(const tg_prefix_attn_args* a) {
+  const tg_kv_cache& c = a->attn.cache;
+  return a->n_groups == 0 ||
+         (long long)(c.B - 1) * c.max_pages * c.page_size * c.Hkv * c.D < 4096ll * 8 * 128;
+}
+
 size_t prefix_attention_workspace_bytes(const tg_prefix_attn_args* a) {
+  if (little(a)) return tree_attention_workspace_bytes(&a->attn);
   size_t bytes;
   carve(a, nullptr, &bytes);
   return bytes;
@@ -487,6 +499,7 @@ size_t prefix_attention_workspace_bytes(const tg_prefix_attn_args* a) {
 
 hipError_t launch_prefix_attention(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
   if (a->attn.T == 0 || a->attn.cache.B == 0) return hipSuccess;
+  if (little(a)) return launch_tree_attention(&a->attn, ws, s);
   return a->attn.cache.dtype == TG_BF16 ? launch_type<Bf16>(a, ws, s) : launch_type<F16>(a, ws, s);
 }
 

@@ -14,15 +14,24 @@ pytestmark = pytest.mark.gpu
 BF, F16 = torch.bfloat16, torch.float16
 
 
-def make(requests, groups, Hq, Hkv, D, dtype, page, seed, layers=2, mask=True, fill=float("nan")):
+def room(B, Hkv, D, page):
+    """Pages per request from which on a call of B requests reads shared pages once:
+    tables that hold less are left to tree attention."""
+    return -(-4096 * 8 * 128 // (max(1, B - 1) * Hkv * D * page))
+
+
+def make(requests, groups, Hq, Hkv, D, dtype, page, seed, layers=2, mask=True, fill=float("nan"),
+         wide=True):
     """requests [(committed tokens, rows)], groups [(first request, requests, shared
     positions)]; pages in no order, those of the shared positions held by all of the
-    group, rows that nobody owns ``fill``."""
+    group, rows that nobody owns ``fill``; tables for ``room`` or (wide False) little
+    more than the requests have."""
     rng = np.random.default_rng(seed)
     L, N = [r[0] for r in requests], [r[1] for r in requests]
     held = [-(-(a + b) // page) for a, b in requests]
     order = rng.permutation(sum(held) + 3)
-    table = np.full((len(requests), max(held + [1]) + 2), -1, np.int32)
+    width = max(max(held + [1]) + 2, room(len(requests), Hkv, D, page) if wide else 0)
+    table = np.full((len(requests), width), -1, np.int32)
     own, at = np.zeros(sum(held) + 3, np.int64), 0  # rows in use of a page
     for b, h in enumerate(held):
         table[b, :h] = order[at:at + h]
@@ -105,6 +114,17 @@ def test_against_float64(requests, groups, Hq, Hkv, D, dtype, page, mask, nodes)
     x = make(requests, groups, Hq, Hkv, D, dtype, page, len(requests) + D + page, mask=mask)
     run(x, groups, Hq, D, max_nodes=nodes)
     run(x, groups, Hq, D, layer=0)  # without max_nodes: the kernels for the mean rows
+
+
+@pytest.mark.parametrize("requests,groups,Hq,Hkv,D,dtype,page,mask,nodes", CASES[1:6])
+def test_small_tables(requests, groups, Hq, Hkv, D, dtype, page, mask, nodes):
+    """So few positions that the call is tree attention: the same bits."""
+    x = make(requests, groups, Hq, Hkv, D, dtype, page, 5, mask=mask, wide=False)
+    got = run(x, groups, Hq, D, max_nodes=nodes).out
+    cache, _, off, L, q, m = x
+    ref = spec.TreeAttention(cache, q, torch.from_numpy(off).to(DEV), ints(L), m,
+                             max_nodes=nodes)(layer=1)
+    assert torch.equal(got.view(torch.int16), ref.view(torch.int16))
 
 
 def test_no_groups_and_no_shared_positions():
@@ -214,6 +234,7 @@ def test_offsets_past_32_bits():
         x.copy_(torch.randn((1, 3, page, 1, D), generator=torch.Generator(DEV).manual_seed(i),
                             device=DEV))
     table = np.tile(np.array([[2, 0, 1, 2, 1, 0, 2, 2, 0, 1]], np.int32), (2, 1))
+    table = np.pad(table, ((0, 0), (0, room(2, 1, D, page))), constant_values=-1)
     cache = spec.KvCache(k, v, torch.from_numpy(table).to(DEV), ints([10, 10]), ints([2, 2, 2]))
     q = torch.randn((2, 3, D), generator=torch.Generator(DEV).manual_seed(5), device=DEV).to(BF)
     x = (cache, table, np.array([0, 1, 2], np.int32), [150, 140], q, None)
@@ -223,7 +244,7 @@ def test_offsets_past_32_bits():
 def test_after_forks_it_gives_what_tree_attention_gives():
     """The pages that KvCache.fork shares, with rows of the requests' own behind."""
     B, P, page = 6, 333, 16
-    cache = spec.KvCache.empty(2, 200, page, 2, 128, B, 40)
+    cache = spec.KvCache.empty(2, 200, page, 2, 128, B, room(B, 2, 128, page))
     lengths, status = ints([0] * B), ints([0] * B)
     slots = ints([0] * P)
     cache.reserve(lengths, ints([0] + [P] * B), slots, status)
