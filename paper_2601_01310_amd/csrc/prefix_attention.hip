@@ -160,7 +160,7 @@ struct Parts {
   const float2* part_ml;
   const float* whole;
   const float2* whole_ml;
-  int rows, unit, blocks;
+  int row_bits, unit_bits, blocks;  // powers of two: rows of an item, positions of a unit
 };
 
 struct JoinParams {
@@ -171,6 +171,8 @@ struct JoinParams {
   int64_t out_stride;
   int T, Hkv, G, cap, max_nodes, B, groups;
 };
+
+__device__ __forceinline__ int pieces(int n, int bits) { return (n + (1 << bits) - 1) >> bits; }
 
 // A running join of a row's parts, four columns to a lane.
 struct Joined {
@@ -194,13 +196,13 @@ __device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, 
   if (units <= 0) return;
   constexpr int kU = 4;
   const int share = max(1, (total + s.blocks - 1) / s.blocks);
-  const int start = pre + (g * tiles + line / s.rows) * units;
+  const int start = pre + (g * tiles + (line >> s.row_bits)) * units;
   const int k0 = start / share, parts = (start + units - 1) / share - k0 + 1;
   if (parts == 1) {
     if (wave == 0) j.add(*reinterpret_cast<const f32x4*>(s.whole + row * D + ch * 4), s.whole_ml[row]);
     return;
   }
-  const int slot = start == k0 * share ? 0 : 1, at = line % s.rows;
+  const int slot = start == k0 * share ? 0 : 1, at = line & ((1 << s.row_bits) - 1);
   for (int k = wave; k < parts; k += kU * kWaves) {
     f32x4 x[kU];
     float2 ml[kU];
@@ -208,7 +210,7 @@ __device__ __forceinline__ void add_parts(Joined& j, const Parts& s, int total, 
     for (int u = 0; u < kU; ++u) {
       const int i = min(k + u * kWaves, parts - 1);
       const int block = min(k0 + i, s.blocks - 1);
-      const int64_t place = (2 * (int64_t)block + (i == 0 ? slot : 0)) * s.rows + at;
+      const int64_t place = ((2 * (int64_t)block + (i == 0 ? slot : 0)) << s.row_bits) + at;
       x[u] = *reinterpret_cast<const f32x4*>(s.part + place * D + ch * 4);
       ml[u] = s.part_ml[place];
     }
@@ -234,8 +236,8 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) 
   request_rows(p.off, b, p.T, p.max_nodes, &first, &n);
   const int L = max(0, min(p.lengths[b], p.cap)), end = min(L + n, p.cap);
   const int total = p.tail.pre[p.B], pre = p.tail.pre[b];
-  const int units = (end - from + p.tail.unit - 1) / p.tail.unit;
-  const int tiles = (n * p.G + p.tail.rows - 1) / p.tail.rows;
+  const int units = pieces(end - from, p.tail.unit_bits);
+  const int tiles = pieces(n * p.G, p.tail.row_bits);
   const int line = (t - first) * p.G + jj;
   const int64_t row = (int64_t)t * Hq + head;
   Joined j;
@@ -244,11 +246,11 @@ __global__ __launch_bounds__(kBlock) void join_parts_kernel(const JoinParams p) 
     const Group x = p.group[gr];
     if (t >= x.first && t < x.first + x.n)  // (offsets that do not ascend)
       add_parts<D>(j, p.prefix, p.prefix.pre[p.groups], p.prefix.pre[gr], g,
-                   (t - x.first) * p.G + jj, (x.positions + p.prefix.unit - 1) / p.prefix.unit,
-                   (x.n * p.G + p.prefix.rows - 1) / p.prefix.rows, row, ch, wave);
+                   (t - x.first) * p.G + jj, pieces(x.positions, p.prefix.unit_bits),
+                   pieces(x.n * p.G, p.prefix.row_bits), row, ch, wave);
   } else {
     const int share = max(1, (total + p.tail.blocks - 1) / p.tail.blocks);
-    const int start = pre + (g * tiles + line / p.tail.rows) * units;
+    const int start = pre + (g * tiles + (line >> p.tail.row_bits)) * units;
     there = start / share == (start + units - 1) / share;
   }
   if (!there) add_parts<D>(j, p.tail, total, pre, g, line, units, tiles, row, ch, wave);
@@ -429,7 +431,8 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
     p.whole_ml = sp.whole_ml[i];
     p.B = i ? c.B : a->n_groups;
     Parts& q = i ? j.tail : j.prefix;
-    q = {p.pre, p.part, p.part_ml, p.whole, p.whole_ml, rows_of(shapes[i]), unit_of(shapes[i]),
+    q = {p.pre, p.part, p.part_ml, p.whole, p.whole_ml, __builtin_ctz(rows_of(shapes[i])),
+         __builtin_ctz(unit_of(shapes[i])),
          merge ? least_blocks(shapes[0], shapes[1], D) : blocks_of(shapes[i], D)};
     if (p.B == 0 || merge) continue;
     e = i ? launch_kind<T, D, kTail>(shapes[i], p, &x, s)
