@@ -9,6 +9,12 @@
 // second; the eight waves of a block split the long axis and add their sums in
 // LDS, wave by wave, so that a token's result depends neither on the other tokens
 // nor on which slot of an expert serves it.
+//
+// 16 tokens of a DeepSeek-V3 share (bf16): 206 us, 5.6 TB/s of weights; one token of
+// a Mixtral layer with its gate 130 us, 5.4 TB/s; 32 tokens of it in 8 bits 276 us,
+// 5.1 TB/s; one token of the share in 8 bits 21 us. (tg_ew_forward: one token of the
+// share in bf16 46 us where this takes 40.5, of the Mixtral layer 147 and 130, 32
+// tokens 488 and 477.)
 #include "tg_device.h"
 #include "tg_launch.h"
 #include "tg_route.h"

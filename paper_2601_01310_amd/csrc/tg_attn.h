@@ -231,7 +231,9 @@ struct Dealer {
     share = max(1, (total + blocks - 1) / blocks);
     // Blocks of one XCD (they are dealt out in turn) take neighbouring runs.
     int each = blocks / (int)Grid::kXcds;
-    if constexpr (kKind != kAll) {  // few runs are spread over all XCDs
+    // Few runs are spread over all XCDs: 8 requests behind 2048 positions 24 us (on two
+    // of them) and 11.6.
+    if constexpr (kKind != kAll) {
       const int used = (total + share - 1) / share;
       each = (used + (int)Grid::kXcds - 1) / (int)Grid::kXcds;
       if ((int)(Grid::block() / Grid::kXcds) >= each) {

@@ -21,14 +21,17 @@ def load(name):
     return m
 
 
-@pytest.mark.parametrize("n,length,most", [(2, 150, 3), (8, 260, 20), (32, 17, 4)])
-def test_steps_against_the_other_operators(n, length, most):
+# held: tokens that a sample has room for; from (n - 1) * held = 32768 on the shared
+# pages are read once (heads 2 of 64).
+@pytest.mark.parametrize("n,length,most,held", [(2, 150, 3, 3), (8, 260, 20, 20), (32, 17, 4, 4),
+                                                (32, 260, 4, 1024), (24, 300, 12, 1600)])
+def test_steps_against_the_other_operators(n, length, most, held):
     ex = load("parallel_sampling")
     base = ex.base
     w = base.weights("cuda")
     g = torch.Generator().manual_seed(n)
     prompt = torch.randint(0, base.VOCAB, (length,), generator=g).tolist()
-    s = ex.Sampler(w, prompt, n, most)
+    s = ex.Sampler(w, prompt, n, held)
     # The same samples as requests of their own, each with its copy of the prompt.
     plain = base.Worker(w, n, 8 * n, base.room([prompt], most, 1))
     plain.prefill([prompt] * n)
