@@ -540,7 +540,7 @@ tg_status tg_tree_attention(const tg_tree_attn_args* a, void* ws, size_t ws_byte
  * tg_tree_attention's up to the last bits; a call without groups, or whose page
  * tables hold so few positions that sharing could save little, is that call.
  * Groups are dealt out by the mean rows of a group, T / n_groups; any are right.
- * The limit is, besides tg_tree_attention's,
+ * The limits are, besides tg_tree_attention's, T < 2^23 and
  *   Hkv * (T * G' + n_groups) * max_pages * page_size / 64 < 2^30.
  */
 typedef struct {
@@ -625,7 +625,7 @@ tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, voi
  * largest float32. A row without tokens gives -1. probs [T, V] float32 (NULL: not
  * wanted; rows probs_stride apart) gets w_i over the mass of all that stay, 0 for
  * the others, and 0 everywhere for a row without tokens. Limits: V <= 2^24,
- * T * ceil(V / 4096) < 2^31; logits aligned to their type.
+ * T * ceil(V / 4096) < 2^23; logits aligned to their type.
  */
 typedef struct {
   int dtype; /* of logits: TG_F32, TG_BF16 or TG_F16 */

@@ -151,6 +151,8 @@ tg_status check_prefix(const tg_prefix_attn_args* a) {
     return set_error(TG_ERR_UNSUPPORTED, "n_groups=%d exceeds 4096", a->n_groups);
   if (a->n_groups > 0 && (!a->group_offsets || !a->shared))
     return set_error(TG_ERR_NULL_ARG, "group_offsets and shared are required");
+  // Threads of the join, 256 to a row, are counted in 32 bits.
+  if (x->T >= 1 << 23) return set_error(TG_ERR_UNSUPPORTED, "T=%d must be below 2^23", x->T);
   // Units of the groups' work, as in check_attn.
   const long long G = x->Hq / x->cache.Hkv;
   const long long items = x->cache.Hkv * (x->T * G / 16 + a->n_groups);
@@ -185,7 +187,8 @@ tg_status check_sample(const tg_sample_args* a) {
   if (a->T < 0 || a->V <= 0)
     return set_error(TG_ERR_BAD_DIM, "T=%d must be >= 0 and V=%d > 0", a->T, a->V);
   if (a->V > (1 << 24)) return set_error(TG_ERR_UNSUPPORTED, "V=%d exceeds 2^24", a->V);
-  if ((long long)a->T * ((a->V + 4095) / 4096) >= (1LL << 31))  // blocks are counted in 32 bits
+  // Threads of a grid, 512 to a block, are counted in 32 bits.
+  if ((long long)a->T * ((a->V + 4095) / 4096) >= (1LL << 23))
     return set_error(TG_ERR_UNSUPPORTED, "T=%d rows of %d logits are too many", a->T, a->V);
   if (a->logits_stride < a->V || (a->probs && a->probs_stride < a->V))
     return set_error(TG_ERR_BAD_DIM, "a row of logits or probabilities is longer than its stride");

@@ -380,7 +380,7 @@ class SampleTokens:
         T, V = logits.shape
         if logits.dtype not in _LOGITS:
             raise ValueError(f"logits is {logits.dtype}, float32, bfloat16 or float16 required")
-        stride = max(V, _rows(logits, "logits", logits.dtype, (V,)))
+        stride = _rows(logits, "logits", logits.dtype, (V,))
         _want(u, "u", torch.float32, (T,))
         _want(temperature, "temperature", torch.float32, (T,), optional=True)
         _want(top_k, "top_k", torch.int32, (T,), optional=True)
@@ -391,7 +391,7 @@ class SampleTokens:
         self.probs = None if probs is False else probs
         probs_stride = V
         if self.probs is not None:
-            probs_stride = max(V, _rows(self.probs, "probs", torch.float32, (V,)))
+            probs_stride = _rows(self.probs, "probs", torch.float32, (V,))
             if self.probs.shape[0] != T:
                 raise ValueError(f"probs has {self.probs.shape[0]} rows, {T} required")
         _same_device(logits, u, temperature, top_k, top_p, min_p, self.probs)

@@ -48,6 +48,8 @@ def sample_args(**kw):
     (dict(attn=attn_args(q=None)), tg.TG_ERR_NULL_ARG),
     (dict(attn=attn_args(c=cache(D=96))), tg.TG_ERR_UNSUPPORTED),
     (dict(attn=attn_args(scale=0.0)), tg.TG_ERR_BAD_DIM),
+    (dict(attn=attn_args(c=cache(B=1, Hkv=1, max_pages=1), T=1 << 23, max_nodes=1, Hq=1)),
+     tg.TG_ERR_UNSUPPORTED),
     # By the requests it could be, as one group it could not.
     (dict(attn=attn_args(c=cache(B=1, max_pages=1 << 20), T=1 << 16, max_nodes=1)),
      tg.TG_ERR_UNSUPPORTED)])
@@ -84,6 +86,8 @@ def test_ew_few_refuses(lib, ew, bad, status):  # noqa: F811
     (dict(V=(1 << 24) + 1, logits_stride=1 << 25, probs_stride=1 << 25), tg.TG_ERR_UNSUPPORTED),
     (dict(T=(1 << 31) - 1, V=1 << 24, logits_stride=1 << 24, probs_stride=1 << 24),
      tg.TG_ERR_UNSUPPORTED),
+    (dict(T=1 << 23, V=1), tg.TG_ERR_UNSUPPORTED), (dict(T=1 << 22, V=4097, logits_stride=5000,
+                                                         probs_stride=5000), tg.TG_ERR_UNSUPPORTED),
     (dict(logits_stride=999), tg.TG_ERR_BAD_DIM), (dict(probs_stride=999), tg.TG_ERR_BAD_DIM),
     (dict(logits=None), tg.TG_ERR_NULL_ARG), (dict(u=None), tg.TG_ERR_NULL_ARG),
     (dict(tokens=None), tg.TG_ERR_NULL_ARG), (dict(logits=P + 2), tg.TG_ERR_UNSUPPORTED),
@@ -107,7 +111,8 @@ def test_what_is_allowed(lib):  # noqa: F811
     assert lib.tg_ew_few_workspace(ctypes.byref(few_args(**F8))) > 0
     for kw in (dict(T=0, logits=None, u=None, tokens=None), dict(V=1), dict(probs=None, probs_stride=0),
                dict(temperature=None, top_k=None, top_p=None, min_p=None),
-               dict(dtype=tg.BF16, logits=P + 2), dict(V=1 << 24, logits_stride=1 << 24, probs=None)):
+               dict(dtype=tg.BF16, logits=P + 2), dict(V=1 << 24, logits_stride=1 << 24, probs=None),
+               dict(T=(1 << 23) - 1, V=1)):
         assert lib.tg_sample_workspace(ctypes.byref(sample_args(**kw))) > 0, kw
 
 

@@ -13,7 +13,7 @@ import math
 import pytest
 import torch
 
-from paper_2601_01310_amd import spec
+from paper_2601_01310_amd import spec, tg
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -265,6 +265,17 @@ def test_strides_and_alignment():
             assert (store[:, :2] == -1).all() and (store[:, 2 + V:] == -1).all()
             ref = make(logits.contiguous(), u, None, None, p)
             assert torch.equal(s.tokens, ref()[0])
+
+
+def test_rows_that_overlap_are_refused():
+    """Expanded rows have a stride of 0 (and a store of them has no place of its own)."""
+    one, u = torch.zeros((1, 50), device=DEV), torch.zeros(3, device=DEV)
+    with pytest.raises(tg.TgError):
+        spec.SampleTokens(one.expand(3, 50), u)
+    with pytest.raises(tg.TgError):
+        spec.SampleTokens(one.expand(3, 50).contiguous(), u, probs=one.expand(3, 50))
+    # Of one row the stride says nothing.
+    assert spec.SampleTokens(one, u[:1])().tolist() == [0]
 
 
 def test_no_rows():
