@@ -25,9 +25,9 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
           "-munsafe-fp-atomics"]
 
 SOURCES = ["gate_topk.hip", "dispatch.hip", "grouped_gemm.hip", "combine.hip", "ew_few.hip",
-           "trigger.hip", "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip", "tree_attention.hip", "prefix_attention.hip",
-           "verify_tree.hip", "sample.hip", "kv_pages.hip",
-           "kv_api.cpp", "tg_api.cpp"]
+           "trigger.hip", "kv_checkpoint.hip", "noalloc.hip", "qk_norm_rope.hip",
+           "tree_attention.hip", "prefix_attention.hip", "verify_tree.hip", "sample.hip",
+           "kv_pages.hip", "kv_api.cpp", "tg_api.cpp"]
 
 
 def _compile(src: str) -> str:
