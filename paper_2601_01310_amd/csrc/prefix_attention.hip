@@ -15,8 +15,8 @@
 //   join    a block takes one to four heads of a row, a wave every fourth part.
 //
 // 128 tokens behind 8192 shared positions and up to 512 of their own (heads 32 / 8
-// of 128, bf16): plan 5 us, prefixes and tails 64, join 10, among other calls 86 (433
-// through each request's own table). The 64 us are neither the memory's (27 us at its
+// of 128, bf16): plan 5 us, prefixes and tails 63, join 10, among other calls 85 (433
+// through each request's own table). The 63 us are neither the memory's (27 us at its
 // rate) nor the matrix unit's (16 % of the time at work): the waves, two of a SIMD,
 // wait in 45 % of theirs, and the vector unit works in 33 %. 16 trees of up to 12
 // rows behind 30000 positions: the prefix's kernel 95 us, 610 TFLOP/s (matrix unit
@@ -26,7 +26,6 @@
 namespace tg {
 namespace {
 
-constexpr int kPlanBlock = 1024, kPlanWaves = kPlanBlock / kWave;
 constexpr int kMaxRequests = 4096;
 constexpr int kWholeUnits = 128;  // positions; a multiple of both kernels' units
 
@@ -51,22 +50,23 @@ __device__ __forceinline__ int last_at(const int* a, int n, int x) {
   return i;
 }
 
-// Every thread has the requests and the groups tid, tid + kPlanBlock and so on; what
-// it reads of them is read at once.
-__global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
-  constexpr int kEach = kMaxRequests / kPlanBlock;
-  __shared__ int starts[kMaxRequests + 1];  // of groups: a request
-  __shared__ int rows[kMaxRequests + 1];    // of requests: a row
-  __shared__ int least[kMaxRequests];       // of a group: its shared positions
-  __shared__ int member[kMaxRequests];      // the first one with rows
-  __shared__ int last[kMaxRequests];        // and the last
+// Every thread has the requests and the groups tid, tid + kThreads and so on, kEach at
+// most; what it reads of them is read at once.
+template <int kThreads, int kEach>
+__global__ __launch_bounds__(kThreads) void plan_kernel(const PlanParams p) {
+  constexpr int kMost = kThreads * kEach, kPlanWaves = kThreads / kWave;
+  __shared__ int starts[kMost + 1];  // of groups: a request
+  __shared__ int rows[kMost + 1];    // of requests: a row
+  __shared__ int least[kMost];       // of a group: its shared positions
+  __shared__ int member[kMost];      // the first one with rows
+  __shared__ int last[kMost];        // and the last
   __shared__ int carry[2][kPlanWaves];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   int first[kEach], next[kEach], length[kEach], group[kEach];
   // Offsets that do not ascend from 0 to B stay inside all arrays.
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int i = k * kPlanBlock + tid;
+    const int i = k * kThreads + tid;
     if (i < p.B) {
       first[k] = p.off[i];
       next[k] = p.off[i + 1];
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int b = k * kPlanBlock + tid;
+    const int b = k * kThreads + tid;
     if (b >= p.B) break;
     int g = p.groups ? last_at(starts, p.groups, b) : -1;
     if (g >= 0 && (b < starts[g] || b >= starts[g + 1])) g = -1;
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   int units[2][kEach] = {};  // of groups, of requests
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int g = k * kPlanBlock + tid;
+    const int g = k * kThreads + tid;
     if (g >= p.groups) break;
     const int shared = member[g] < last[g] ? least[g] / kWholeUnits * kWholeUnits : 0;
     least[g] = shared;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int b = k * kPlanBlock + tid;
+    const int b = k * kThreads + tid;
     if (b >= p.B) break;
     const int from = group[k] >= 0 ? least[group[k]] : 0;
     p.from[b] = from;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
   int base[2] = {0, 0};
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    if (k * kPlanBlock >= max(p.B, p.groups)) break;
+    if (k * kThreads >= max(p.B, p.groups)) break;
     int x[2] = {units[0][k], units[1][k]};
     for (int m = 1; m < kWave; m *= 2) {
       const int o[2] = {__shfl_up(x[0], m), __shfl_up(x[1], m)};
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
     if (k) __syncthreads();
     if (lane == kWave - 1) carry[0][wave] = x[0], carry[1][wave] = x[1];
     __syncthreads();
-    const int i = k * kPlanBlock + tid;
+    const int i = k * kThreads + tid;
     for (int j = 0; j < 2; ++j) {
       int front = base[j];
       for (int w = 0; w < kPlanWaves; ++w) {
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(kPlanBlock) void plan_kernel(const PlanParams p) {
     }
   }
   if (tid == 0) p.pre_prefix[0] = p.pre_tail[0] = 0;
-  for (int t = tid; t < p.T; t += kPlanBlock) {
+  for (int t = tid; t < p.T; t += kThreads) {
     const int b = last_at(rows, p.B, t);
     p.request_of_row[t] = t >= rows[b] && t < min(rows[b + 1], rows[b] + p.max_nodes) ? b : -1;
   }
@@ -422,7 +422,11 @@ hipError_t launch(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
   plan.group_of = sp.group_of;
   plan.request_of_row = sp.request_of_row;
   plan.group = sp.group;
-  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanBlock), 0, s, plan);
+  // Fewer waves wait for each other sooner: 61 requests 3.8 us, by 16 waves 4.5.
+  if (c.B <= 256 && a->n_groups <= 256 && x.T <= 1024)
+    hipLaunchKernelGGL((plan_kernel<256, 1>), dim3(1), dim3(256), 0, s, plan);
+  else
+    hipLaunchKernelGGL((plan_kernel<1024, kMaxRequests / 1024>), dim3(1), dim3(1024), 0, s, plan);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   JoinParams j;
