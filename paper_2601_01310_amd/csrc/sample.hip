@@ -20,7 +20,7 @@
 //
 // 128 rows of 128000 tokens, bf16, temperature alone: part 17.6 us, draw 6, 22 in
 // all (5.2 to read the logits); float32 with filters of all kinds: part 19, cut 9,
-// keep 21, draw 16, 60 in all. part and keep are bound by the vector unit, which
+// keep 21, draw 16, 60 to 67 in all. part and keep are bound by the vector unit, which
 // forms a weight in about 33 instructions and issues in 70 to 90 % of the time;
 // cut and draw by their chains of barriers, one block to a row.
 #include "tg_kv.h"
