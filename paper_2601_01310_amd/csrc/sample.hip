@@ -39,7 +39,11 @@ constexpr int kDigits = 2048;     // of the radix selection
 constexpr int kList = 3328;       // listed tokens of a row and border
 constexpr int kPartList = 768;    // of a part
 constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / kWave;
-constexpr uint32_t kOverflow = 1u << 24;
+// What a part whose tokens do not fit adds to their count: more than the list holds,
+// and little enough that no number of parts comes to 2^32.
+constexpr uint32_t kOverflow = kList + 1;
+static_assert(kOverflow > kPartList && (1ull << 24) / kPart * kOverflow < 1ull << 32,
+              "the tokens of all parts are counted in 32 bits");
 constexpr int kFoldParts = 8;
 
 typedef unsigned long long u64;
@@ -64,7 +68,7 @@ struct Space {
   u64* mass;        // [T][parts][kSteps]
   uint32_t* count;  // [T][parts][kSteps]
   CutInfo* cut;     // [T]
-  uint32_t* listed; // [T][2] of the next two lists; kOverflow and more: not all
+  uint32_t* listed; // [T][2] of the next two lists; more than kList: not all are there
   u64* list_k;      // [T][kList]
   u64* list_p;      // [T][kList]
 };
@@ -997,6 +1001,7 @@ __global__ __launch_bounds__(kDrawBlock) void draw_kernel(const uint8_t* __restr
   for (int i = 0; i < kPer; ++i) own += sh.bucket[tid * kPer + i];
   u64 upto = own;
   scan<kDrawWaves>(sh.scan, sh.scan_n, &upto, (uint32_t*)nullptr, &whole);
+  // (The likeliest token stays whatever the filters are: whole is not 0.)
   const u64 to = min(share_of(p.u[t], whole, false), whole - 1);
   if (upto > to && upto - own <= to) {
     u64 at = upto - own;

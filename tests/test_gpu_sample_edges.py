@@ -1,0 +1,76 @@
+"""tg_sample on the GPU at the edges of its range: rows whose border holds more tokens
+than the lists, logits of every bit pattern. Expected values follow from the definition
+in whole numbers and float64."""
+import math
+from fractions import Fraction
+
+import pytest
+import torch
+
+from paper_2601_01310_amd import spec
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def border(k, p, m, n, ratio):
+    """How many of m tokens of weight 1 and n of weight ``ratio`` (Fraction) behind
+    them top-k and then top-p keep, from the definition in whole numbers."""
+    m, n = min(k, m), min(max(k - m, 0), n)
+    if p >= 1:
+        return m + n
+    to = p * (m + n * ratio)  # a token stays if the mass before it is less
+    if to <= m:
+        return math.ceil(to)
+    if ratio < 1:  # weights are rounded: not at a border (see the test)
+        at = (to - m) / ratio
+        assert 2.0 ** -8 < at - math.floor(at) < 1 - 2.0 ** -8
+    return m + min(n, math.ceil((to - m) / ratio))
+
+
+@pytest.mark.parametrize("filters", ["k", "p", "kp"])
+@pytest.mark.parametrize("V,dtype", [(1 << 20, "f32"), (1 << 20, "bf16"), ((1 << 20) + 5, "f32"),
+                                     (3 << 20, "f16"), (1 << 24, "f32"), (1 << 24, "bf16")])
+def test_flat_rows_of_256_parts_and_more(V, dtype, filters):
+    """Rows of one and of two levels, all of whose parts have more tokens at the
+    border than they can list.
+
+    Weights of one level are equal, and so whatever is counted is exact. Those of the
+    lower level are within half a unit of 2^-s and 2^-42 of themselves, s >= 38 and
+    e^-1 > 2^-2: 2^-36 together. Up to 2^24 of them move a border by less than 2^-8
+    tokens, and a probability by less than 2^-34 of itself beside its rounding."""
+    print(f"[gpu] sample, flat rows, V={V} {dtype} {filters}", flush=True)
+    low = Fraction(math.exp(-1.0))  # of the upper level's weight, to 2^-53
+    logits = torch.full((4, V), 0.5, device=DEV, dtype=DTYPES[dtype])
+    logits[1] -= 1.0  # and rows of two levels:
+    logits[2:] = 0.0
+    logits[2, 13::97] = 1.0
+    logits[3, V - 3:] = 1.0
+    ks = [3, V - 1, V // 2, 5000] if "k" in filters else [V] * 4
+    ps = [0.5, 0.3, 0.7, 0.999] if "p" in filters else [1.0] * 4
+    us = [0.75, 0.999, 0.4, 0.6]
+    k = torch.tensor(ks, dtype=torch.int32, device=DEV) if "k" in filters else None
+    p, u = (torch.tensor(x, device=DEV) for x in (ps, us))
+    s = spec.SampleTokens(logits, u, None, k, p if "p" in filters else None, probs=True)
+    s.tokens.fill_(-7)
+    s.probs.fill_(float("nan"))
+    tokens, probs = s()
+    for t in range(4):
+        top = logits[t] == logits[t].max()
+        m, ratio = int(top.sum()), low if t >= 2 else Fraction(1)
+        n = border(ks[t], Fraction(float(p[t])), m, V - m, ratio)
+        at = torch.where(top, torch.cumsum(top, 0), m + torch.cumsum(~top, 0))  # from 1
+        kept = at <= n
+        w = torch.where(top, 1.0, float(ratio)).double() * kept
+        whole = float(w.sum())
+        assert torch.equal(probs[t] > 0, kept), (t, n, int((probs[t] > 0).sum()))
+        err = (probs[t].double() * whole - w).abs()
+        assert bool((err <= w * (2.0 ** -24 + 2.0 ** -33)).all()), (t, float(err.max()))
+        x, i = float(u[t]), int(tokens[t])
+        if t < 2:
+            assert i == math.floor(Fraction(x) * n), (t, i, n)
+        else:
+            upto, slack = torch.cumsum(w, 0), V * 2.0 ** -36
+            assert bool(kept[i]) and float(upto[i]) > x * whole - slack, (t, i)
+            assert float(upto[i] - w[i]) <= x * whole + slack, (t, i)
