@@ -111,12 +111,14 @@ struct Of<Bf16> : Of16<Bf16> {};
 template <>
 struct Of<F16> : Of16<F16> {};
 
-// NaN is no token's logit, infinity the largest finite one: the median of three, of
-// which the instruction gives the least if one is NaN (the compiler, which makes a
-// minimum of the builtin, would give the other bound).
+// NaN is no token's logit, infinity the largest finite one: the median of three. With a
+// NaN among them the instruction gives the least of the three by two minima in turn, of
+// which the first makes a signalling NaN a quiet one and the second leaves that out:
+// -infinity has to be the last operand. (The compiler, which makes a minimum of the
+// builtin, would give the other bound.)
 __device__ __forceinline__ float clean(float x) {
   float y;
-  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "v"(-INFINITY), "v"(3.402823466e38f));
+  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(y) : "v"(x), "v"(3.402823466e38f), "v"(-INFINITY));
   return y;
 }
 

@@ -74,3 +74,41 @@ def test_flat_rows_of_256_parts_and_more(V, dtype, filters):
             upto, slack = torch.cumsum(w, 0), V * 2.0 ** -36
             assert bool(kept[i]) and float(upto[i]) > x * whole - slack, (t, i)
             assert float(upto[i] - w[i]) <= x * whole + slack, (t, i)
+
+
+BITS = {  # NaN: signalling and quiet ones, of both signs, least and largest payloads
+    "f32": (torch.int32, (0x7F800001, 0x7FBFFFFF, 0xFF800001, 0xFFBFFFFF, 0x7FC00000, 0xFFFFFFFF)),
+    "bf16": (torch.int16, (0x7F81, 0x7FBF, 0xFF81, 0xFFBF, 0x7FC0, 0xFFFF)),
+    "f16": (torch.int16, (0x7C01, 0x7DFF, 0xFC01, 0xFDFF, 0x7E00, 0xFFFF)),
+}
+
+
+@pytest.mark.parametrize("dtype", list(BITS))
+@pytest.mark.parametrize("V", [3, 1000, 9001])
+def test_no_nan_is_a_token(V, dtype):
+    """A logit of any NaN's bits counts as -infinity's does, in whole vectors and at a
+    row's end, with and without filters and for the likeliest token."""
+    print(f"[gpu] sample, NaN, V={V} {dtype}", flush=True)
+    kind, codes = BITS[dtype]
+    bits = 8 * torch.empty((), dtype=kind).element_size()
+    codes = [c - (1 << bits) if c >> (bits - 1) else c for c in codes]
+    T, g = len(codes) + 1, torch.Generator(DEV).manual_seed(V)
+    logits = torch.randn((T, V), generator=g, device=DEV).to(DTYPES[dtype])
+    ref = logits.clone()
+    gone = torch.rand((T, V), generator=g, device=DEV) < 0.3
+    gone[:, -1] = True
+    gone[:, 1] = False
+    gone[T - 1] = True
+    ref[gone] = -math.inf
+    for t in range(T):
+        logits[t].view(kind)[gone[t]] = codes[t % len(codes)]
+    assert bool(logits[gone].isnan().all()) and not logits[~gone].isnan().any()
+    u = torch.rand(T, generator=g, device=DEV)
+    full = lambda x, kind=torch.float32: torch.full((T,), x, dtype=kind, device=DEV)  # noqa: E731
+    for f in ((None,) * 4, (full(0.0), None, None, None), (full(0.7), full(20, torch.int32), None, None),
+              (None, None, full(0.8), None), (None, None, None, full(0.1)),
+              (full(1.3), full(30, torch.int32), full(0.9), full(0.01))):
+        a, b = (spec.SampleTokens(x, u, *f, probs=True)() for x in (logits, ref))
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        assert not a[1][gone].any() and int(a[0][T - 1]) == -1
+        assert bool((~gone[:T - 1].gather(1, a[0][:T - 1, None].long())).all())
