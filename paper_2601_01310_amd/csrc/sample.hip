@@ -687,8 +687,11 @@ struct Border {
 
 // Any border. Of its tokens in the order of their keys, with `before` tokens and
 // `before_mass` before them all: those from `cut` on with fewer than `most` tokens
-// and less than `mass` before them. Returns the key from which on they stay (`cut`
-// if all do), the mass before it and its own in *kept.
+// and less than `mass` before them. Returns the key from which on they stay, the mass
+// before it and its own in *kept. If all of the border do, that is their last one's: the
+// border ends at it, and what is less likely never stays. (A step's tokens, each in whole
+// units of the row, may come to less than their mass in the smaller units of their parts,
+// by which the border's steps were found.)
 template <class T>
 __device__ __attribute__((noinline)) u64 select(DrawShared& sh, const Border<T>& border, u64 cut,
                                                 uint32_t before, u64 before_mass, uint32_t most,
@@ -769,7 +772,7 @@ __device__ __attribute__((noinline)) u64 select(DrawShared& sh, const Border<T>&
     if (digit < 0) {  // all of them stay (or none)
       if (!stays(0, 0)) return ~0ull;
       *kept = before_mass + all;
-      return cut;
+      return max(cut, lo);
     }
     before += sh.before;
     before_mass += sh.before_mass;

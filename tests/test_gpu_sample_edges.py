@@ -1,6 +1,6 @@
 """tg_sample on the GPU at the edges of its range: rows whose border holds more tokens
-than the lists, logits of every bit pattern. Expected values follow from the definition
-in whole numbers and float64."""
+than the lists, logits of every bit pattern, tails of small weights. Expected values
+follow from the definition in whole numbers and float64."""
 import math
 from fractions import Fraction
 
@@ -112,3 +112,28 @@ def test_no_nan_is_a_token(V, dtype):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
         assert not a[1][gone].any() and int(a[0][T - 1]) == -1
         assert bool((~gone[:T - 1].gather(1, a[0][:T - 1, None].long())).all())
+
+
+def test_nothing_stays_behind_the_border():
+    """A long tail of weights of a few units: rounded to these, the tokens of the
+    border's step come to less than the share that their masses before the rounding
+    gave, and all of them stay. Those behind them do not.
+
+    V = 2^19, s = 43, and the likeliest token's weight is 2^43 units. n tokens have 4.4
+    units (4, rounded) and n, less likely, 2.4 (2). top_p = 1 - 2^-24 leaves out
+    2^19 = 524288 units, more than the latter have together (483958), so none of them
+    stays."""
+    print("[gpu] sample, tails of small weights", flush=True)
+    V, n = 1 << 19, 201649
+    logits = torch.full((1, V), -math.inf, device=DEV)
+    at = torch.randperm(V, generator=torch.Generator(DEV).manual_seed(3), device=DEV)
+    top, some, rest = at[:1], at[1:n + 1], at[n + 1:2 * n + 1]
+    logits[0, top] = 0.0
+    logits[0, some] = -math.log(2.0) * (43 - math.log2(4.4))
+    logits[0, rest] = -math.log(2.0) * (43 - math.log2(2.4))
+    p = torch.full((1,), 1 - 2.0 ** -24, device=DEV)
+    for u in (0.5, 1 - 2.0 ** -24):
+        token, probs = spec.SampleTokens(logits, torch.full((1,), u, device=DEV), top_p=p, probs=True)()
+        assert not probs[0, rest].any(), int(probs[0, rest].count_nonzero())
+        assert float(probs[0, top]) > 0.5 and probs[0, some].any()
+        assert float(probs[0, int(token)]) > 0
