@@ -124,7 +124,10 @@ template <bool kF8, int kM, int kQ, int kRing, class At, class Done>
 __device__ __forceinline__ void stream(uint16_t* lds, int row_bytes, int runs, At at, Done done) {
   constexpr int kEl = kF8 ? 128 : 64;  // elements per step
   constexpr int kB = kEl / 32;         // operands of the other rows per step
-  constexpr int kLoads = 2 * kM + kQ * kB + (kF8 ? kM : 0);
+  // Loads of a step that are vector loads whatever the compiler does: 16 bytes a lane
+  // from addresses of its own. It may take scales, the same for many lanes, as scalar
+  // ones, which a wait for vector loads must not count.
+  constexpr int kLoads = 2 * kM + kQ * kB;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id(), col = lane & 15, quad = lane >> 4;
   const int steps = row_bytes / kStep;
