@@ -30,7 +30,7 @@ constexpr int kCols = 16;      // token rows per operand
 constexpr int kTableInts = 2048;  // a routing table up to this size is kept in LDS
 constexpr int kStep = 128;     // bytes of a weight row per step
 constexpr int kStage = 16 * kStep / 2;  // 16-bit elements of 16 rows' step in LDS
-constexpr int kGateLogits = 64;  // a block forms up to so many logits itself
+constexpr int kGateLogits = 16;  // every block forms up to so many logits itself
 // Up to so many tokens the second kernel forms the sums, with runs of 16 weight rows;
 // above, a third one does, and runs may be taller. 16 tokens of a Mixtral layer in 8
 // bits take 273 us the first way and 259 the second, 8 tokens 264 and 268, of a
@@ -770,7 +770,7 @@ hipError_t launch_ew_few(const tg_ew_few_args* a, void* ws, hipStream_t s) {
   p.plan = L.plan;
   // Few logits are formed by every block for itself, which saves a launch: one token
   // of 8 experts of 4096, 136 us with a gate kernel before, 130 without.
-  if (!e.logits_in && (long long)e.T * e.E <= kGateLogits / 4) {
+  if (!e.logits_in && (long long)e.T * e.E <= kGateLogits) {
     p.w_gate = e.w_gate;
   } else if (!e.logits_in) {
     if (e.topk_w) p.plan.w = e.topk_w;
