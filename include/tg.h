@@ -252,6 +252,8 @@ tg_status tg_ew_forward_noalloc(const tg_ew_args* a, void* stream);
  *
  * ew.slot_counts, slot_offsets, pair_row and y must be NULL: nothing is permuted,
  * and a few tokens are forwarded again rather than replayed.
+ * Every workgroup reads ert and slot_alive for itself: they must not change while the
+ * call runs.
  */
 #define TG_MAX_FEW 32
 #define TG_MAX_FEW_PAIRS 256
@@ -621,11 +623,13 @@ tg_status tg_verify_tree(const tg_verify_args* a, void* ws, size_t ws_bytes, voi
  * Weights are exact to 2^-42 of themselves and counted in units of at most
  * 2^(1 - s), s = min(45, 62 - ceil(log2 V)); what is less counts for nothing. Their
  * sums and shares of them are exact, and a row's result does not depend on the
- * other rows. Logits of -infinity or NaN are no tokens, +infinity counts as the
- * largest float32. A row without tokens gives -1. probs [T, V] float32 (NULL: not
- * wanted; rows probs_stride apart) gets w_i over the mass of all that stay, 0 for
- * the others, and 0 everywhere for a row without tokens. Limits: V <= 2^24,
- * T * ceil(V / 4096) < 2^23; logits aligned to their type.
+ * other rows. (The mass that top_p is a share of is summed in smaller units, and so
+ * may be less or more than the sum of the weights by up to two units a token.) Logits
+ * of -infinity or NaN are no tokens, +infinity counts as the largest float32. A row
+ * without tokens gives -1. probs [T, V] float32 (NULL: not wanted; rows probs_stride
+ * apart) gets w_i over the mass of all that stay, 0 for the others, and 0 everywhere
+ * for a row without tokens. Limits: V <= 2^24, T * ceil(V / 4096) < 2^23; logits
+ * aligned to their type.
  */
 typedef struct {
   int dtype; /* of logits: TG_F32, TG_BF16 or TG_F16 */

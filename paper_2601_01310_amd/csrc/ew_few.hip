@@ -14,7 +14,9 @@
 // a Mixtral layer with its gate 130 us, 5.4 TB/s; 32 tokens of it in 8 bits 276 us,
 // 5.1 TB/s; one token of the share in 8 bits 21 us. (tg_ew_forward: one token of the
 // share in bf16 46 us where this takes 40.5, of the Mixtral layer 147 and 130, 32
-// tokens 488 and 477.)
+// tokens 488 and 477.) Layers of small d lose by the second kernel, up to 16 tokens of
+// which have d / 16 blocks: 8 tokens with I = 8192 and 7 experts touched, d = 512 60 us
+// (tg_ew_forward 52), 1024 91 (83), 2048 137 (175).
 #include "tg_device.h"
 #include "tg_launch.h"
 #include "tg_route.h"
@@ -35,7 +37,8 @@ constexpr int kGateLogits = 16;  // every block forms up to so many logits itsel
 // above, a third one does, and runs may be taller. 16 tokens of a Mixtral layer in 8
 // bits take 273 us the first way and 259 the second, 8 tokens 264 and 268, of a
 // DeepSeek-V3 share 86 and 93; in bf16 the first is the faster one up to 16 tokens
-// (share 205 and 208 us).
+// (share 205 and 208 us). (d is 4096 and 7168 there; for smaller ones the border, which
+// goes by tokens alone, is not measured.)
 template <bool kF8>
 constexpr int fused_tokens() {
   return kF8 ? 8 : 16;

@@ -17,10 +17,10 @@
 // 128 tokens behind 8192 shared positions and up to 512 of their own (heads 32 / 8
 // of 128, bf16): plan 5 us, prefixes and tails 63, join 10, among other calls 85 (433
 // through each request's own table). The 63 us are neither the memory's (27 us at its
-// rate) nor the matrix unit's (16 % of the time at work): the waves, two of a SIMD,
-// wait in 45 % of theirs, and the vector unit works in 33 %. 16 trees of up to 12
-// rows behind 30000 positions: the prefix's kernel 95 us, 610 TFLOP/s (matrix unit
-// 32 %, vector unit 44 %, waits 37 %), tails 13, join 11.
+// rate) nor the matrix unit's (16 % of the time at work): the prefixes have half of the
+// device (see both_kernel), and their 17.2 GFLOP would take it 56 us at half of the next
+// case's rate. 16 trees of up to 12 rows behind 30000 positions: the prefix's kernel 95
+// us, 610 TFLOP/s (matrix unit 32 %, vector unit 44 %, waits 37 %), tails 13, join 11.
 #include "tg_attn.h"
 
 namespace tg {
@@ -320,9 +320,9 @@ Space carve(const tg_prefix_attn_args* a, char* base, size_t* bytes) {
   return s;
 }
 
-// Both in one launch, for tails of at most 16 rows a KV head: every other block
-// takes prefixes, which the products and the vector unit bound, or tails, which the
-// memory does, so that each CU has both at once. (One launch less: 128 requests
+// Both in one launch, for tails of at most 16 rows a KV head: every other block takes
+// prefixes, the others tails. Blocks go to the XCDs in turn, so prefixes have four of
+// the eight and tails the other four, and no CU has both. (One launch less: 128 requests
 // behind 8192 tokens 100 us instead of 104, four behind 1000, a case now left to tree
 // attention, 21 instead of 30.)
 template <class T, int D, int kPrefixQ, bool kShared, int kPagesOf, int kOcc>
@@ -500,7 +500,9 @@ hipError_t launch_type(const tg_prefix_attn_args* a, void* ws, hipStream_t s) {
 // join cost more, by what the page tables can hold: heads 32 / 8 of 128, bf16, one
 // token each behind 200 tokens of their own, tree attention and this one (us): 4
 // requests behind 1000 shared positions 12.6 and 17.2, 8 behind 512 11.9 and 17.5; 4
-// behind 2048 20.0 and 17.3, 8 behind 2048 21.5 and 18.9.
+// behind 2048 20.0 and 17.3, 8 behind 2048 21.5 and 18.9. Tables that can hold more than
+// their requests have are taken for long ones: 32 behind 128 16.2 and 23.4, 32 behind 512
+// 19.6 and 24, and the first two with tables for 8704 positions take the longer way too.
 static bool little(const tg_prefix_attn_args* a) {
   const tg_kv_cache& c = a->attn.cache;
   return a->n_groups == 0 ||

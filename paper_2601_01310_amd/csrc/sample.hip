@@ -36,14 +36,24 @@ constexpr int kSteps = 512;       // eighths of a power of two
 constexpr int kNone = kSteps - 1;  // what is too small for a weight
 constexpr int kBuckets = 1024;    // masses in token order, of the draw
 constexpr int kDigits = 2048;     // of the radix selection
-constexpr int kList = 3328;       // listed tokens of a row and border
-constexpr int kPartList = 768;    // of a part
+// Listed tokens of a row and border (what the draw's other tables leave of 64 KB of LDS),
+// and of a part (12 KB, so that LDS holds more blocks of keep_kernel than a CU takes).
+// Past either the draw's one block goes through the row itself, several times: 128 rows
+// of 256000 tokens of deviation 2.5, top-p 0.95, 124 us at temperature 1 and 3700 at 1.3;
+// of 128000 tokens 81 us at 1.75 and 1280 at 2.
+constexpr int kList = 3328;
+constexpr int kPartList = 768;
 constexpr int kDrawBlock = 256, kDrawWaves = kDrawBlock / kWave;
 // What a part whose tokens do not fit adds to their count: more than the list holds,
 // and little enough that no number of parts comes to 2^32.
 constexpr uint32_t kOverflow = kList + 1;
 static_assert(kOverflow > kPartList && (1ull << 24) / kPart * kOverflow < 1ull << 32,
               "the tokens of all parts are counted in 32 bits");
+// Rows of up to so many parts have no kernel for the cut: every block of keep_kernel finds
+// it for itself, which saves a launch and repeats the work. 1 and 8 rows of 16384 tokens
+// (4 parts), all filters, 23.1 and 23.3 us (26.2 and 26.0 with the kernel), of 32003 (8
+// parts) 22.9 and 24.9 (24.3 and 25.9), of 64000 (16 parts) 25.6 and 27.8 (25.7 and 27.2).
+// Batches lose by it: 64 and 192 rows of 32003 31.8 and 47.9 us (28.7 and 38.7).
 constexpr int kFoldParts = 8;
 
 typedef unsigned long long u64;

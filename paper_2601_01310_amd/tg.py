@@ -25,8 +25,8 @@ EXPORTS = [
     "tg_ew_few_workspace", "tg_ew_few",
     "tg_ew_replay_workspace", "tg_ew_replay", "tg_batch_trigger", "tg_kv_checkpoint",
     "tg_kv_checkpoint_strided", "tg_kv_restore", "tg_qk_norm_rope", "tg_tree_attention_workspace",
-    "tg_tree_attention", "tg_prefix_attention_workspace", "tg_prefix_attention", "tg_verify_tree_workspace", "tg_verify_tree", "tg_sample_workspace",
-    "tg_sample", "tg_kv_compact",
+    "tg_tree_attention", "tg_prefix_attention_workspace", "tg_prefix_attention",
+    "tg_verify_tree_workspace", "tg_verify_tree", "tg_sample_workspace", "tg_sample", "tg_kv_compact",
     "tg_kv_pages_reserve", "tg_kv_pages_fork", "tg_kv_pages_trim",
 ]
 
@@ -177,8 +177,7 @@ def load(path: Optional[str] = None):
     lib.tg_qk_norm_rope.restype = i
     lib.tg_qk_norm_rope.argtypes = [ctypes.POINTER(QkArgs), vp]
     for name, args in (("tg_tree_attention", TreeAttnArgs), ("tg_prefix_attention", PrefixAttnArgs),
-                       ("tg_verify_tree", VerifyArgs),
-                       ("tg_sample", SampleArgs)):
+                       ("tg_verify_tree", VerifyArgs), ("tg_sample", SampleArgs)):
         size, call = getattr(lib, name + "_workspace"), getattr(lib, name)
         size.restype, size.argtypes = sz, [ctypes.POINTER(args)]
         call.restype, call.argtypes = i, [ctypes.POINTER(args), vp, sz, vp]
